@@ -337,6 +337,96 @@ VECTOR_API vector_status vector_decode_attn_layer(const vector_shape* shape, con
                                                   size_t ws_bytes, void* stream);
 
 /*
+ * ---- The mixed cache in 4 bits and pages ----------------------------------------------------------
+ * What a server holds that keeps many sequences: rows of the mixed cache in 4 bits, in pages that sequences of different lengths
+ * take and give back.  (The paper has no counterpart; what is attended to is the same, with rows rounded.)
+ *
+ *  - A row is held in microscaled 4-bit floating point: 16 neighbouring channels share a scale s, the smallest number of
+ *    five exponent bits (bias 15) and three mantissa bits with 6 s >= max |x|; a channel is the nearest of
+ *    {0, 1/2, 1, 3/2, 2, 3, 4, 6} s with its sign, ties to the even code.  72 bytes a row of 128 channels, 36 of 64.
+ *    s is at most 10240 (what is larger than 61440 is cut off there, infinities too) and at least 2^-17; a group that holds a NaN reads as NaN.
+ *  - A page holds VECTOR_PAGE_ROWS rows of every (layer, KV head).  A sequence has one list of pages per tier, a row of that tier's table,
+ *    shared by its layers and heads: row r of the sequence lies in page table[b][r / 64] at row r % 64.  A slot, page * 64 + row, names a place.
+ *    Pools: ret_pages [n_ret_pages][L * Hkv][2][tile], the keys and then the values of retained rows, and apx_pages
+ *    [n_apx_pages][L * Hkv][tile], the keys of key-only rows, tile = vector_q4_tile_bytes().  All device memory, caller-owned,
+ *    at multiples of 16 bytes; what lies behind a sequence's last row may be anything.
+ *  - Rows, queries and maps of these calls lie at multiples of 16 bytes (else VECTOR_ERR_SHAPE); at most VECTOR_Q4_MAX_BATCH
+ *    sequences in a call of vector_decode_attn_q4.
+ */
+#define VECTOR_PAGE_ROWS 64
+#define VECTOR_Q4_MAX_BATCH 1024
+typedef struct {
+    void*          ret_pages;
+    void*          apx_pages;
+    const int32_t* ret_table;    /* [batch][ret_width] pages of each sequence                */
+    const int32_t* apx_table;    /* [batch][apx_width]                                       */
+    const int32_t* ret_len;      /* [batch] rows of each sequence, on the device             */
+    const int32_t* apx_len;      /* [batch]                                                  */
+    int32_t*       ret_pos;      /* [n_ret_pages][L * Hkv][64] original token index, or NULL */
+    int32_t*       apx_pos;      /* [n_apx_pages][L * Hkv][64], or NULL where rope is off    */
+    int64_t        n_ret_pages, n_apx_pages;      /* fewer than 2^25 each                    */
+    int32_t        ret_width, apx_width;
+} vector_q4_cache;
+
+/* Bytes of a page's 64 rows of one (layer, KV head): 4608 for 128 channels, 2304 for 64; 0 for an unsupported shape. */
+VECTOR_API size_t vector_q4_tile_bytes(const vector_shape* shape);
+
+/*
+ * Page tables, lengths and slots after requests grew, shrank or ended, on the device from their lengths alone.  Request b has lengths[b] rows, in the
+ * pages that the first ceil(lengths[b] / page_rows) entries of its row of the table name, and changes by added[b] rows:
+ *  - added[b] < 0: its last rows go (all of them where it has no more), and pages that hold none of the rest are pushed on the stack free_pages, requests in
+ *    order and a request's pages in order.  The table's entries stay as they are behind a request's pages.
+ *  - added[b] > 0: it takes the pages that it lacks from the top of the stack, after all pushes, requests in order.  Where the stack runs out, or the
+ *    table's row is full, the request gets as many rows as its pages hold.
+ * new_lengths[b]: the rows that it has then; first_row[b]: those that it had; row_start[b]: the sum of the positive changes before b, so that row_start[batch]
+ * is all added rows; slots[row_start[b] + i]: the slot of its i-th added row, -1 where it got no page for it; slots behind the last added row are -1.  new_n_free:
+ * the pages that are left on the stack.  new_lengths may be lengths, and new_n_free may be n_free; no other two of the buffers may overlap.
+ * All device int32: lengths, added, new_lengths, first_row [batch], row_start [batch + 1], table [batch][width], free_pages [cap_free], n_free and
+ * new_n_free [1], slots [n_slots] (NULL if n_slots is 0; rows beyond n_slots have no slot written).  A negative length counts as none, a length beyond the table
+ * as a full one.  batch <= 65535, width * page_rows < 2^31, and so the sum of the positive changes.
+ */
+VECTOR_API vector_status vector_block_tables(int32_t batch, const int32_t* lengths, const int32_t* added, int32_t page_rows,
+                                             int32_t* table, int32_t width, int32_t* free_pages, int32_t cap_free, const int32_t* n_free,
+                                             int32_t* new_lengths, int32_t* new_n_free, int32_t* first_row, int32_t* row_start,
+                                             int32_t* slots, int64_t n_slots, void* stream);
+
+/*
+ * vector_compact into pages: rows ret_idx of K and V and rows apx_idx of K, rounded to 4 bits, go to the slots ret_slots (device [batch][n_ret]) and
+ * apx_slots (device [batch][n_apx]) of the pools, their token indices to ret_pos and apx_pos where those are not NULL.  The slots of a call
+ * are all different.  A token index outside the context, or a slot outside the pool (-1), skips the row.  Tables and lengths are not used.
+ */
+VECTOR_API vector_status vector_compact_q4(const vector_shape* shape, const vector_budget* budget, const void* K, const void* V,
+                                           const int32_t* ret_idx, const int32_t* apx_idx, const vector_q4_cache* cache,
+                                           const int32_t* ret_slots, const int32_t* apx_slots, void* stream);
+
+/*
+ * vector_append into pages: the rows of one generated token of every sequence, k_new and v_new (device [U][d]), rounded to 4 bits, go to slot
+ * slots[row_start[b]] of the retained pool (row_start, slots: as vector_block_tables wrote them; a sequence with no new row has none written), or to slots[b] where
+ * row_start is NULL; pos[b] (device; may be NULL where ret_pos is) becomes the row's entry of ret_pos.  A slot outside the pool, or a place outside the
+ * n_slots slots, skips the row.
+ */
+VECTOR_API vector_status vector_append_q4(const vector_shape* shape, const vector_q4_cache* cache, const void* k_new, const void* v_new,
+                                          const int32_t* row_start, const int32_t* slots, int64_t n_slots, const int32_t* pos, void* stream);
+
+/*
+ * Rows read back as the values that they stand for: slots ret_slots (device [batch][n_ret]) to ret_k and ret_v (device [U][n_ret][d] of shape->dtype, which
+ * holds the values exactly), slots apx_slots (device [batch][n_apx]) to apx_k (device [U][n_apx][d]).  A slot outside the pool gives zeros.
+ */
+VECTOR_API vector_status vector_read_q4(const vector_shape* shape, const vector_q4_cache* cache, const int32_t* ret_slots, int64_t n_ret,
+                                        void* ret_k, void* ret_v, const int32_t* apx_slots, int64_t n_apx, void* apx_k, void* stream);
+
+/* Bytes of device workspace that vector_decode_attn_q4 needs for this shape, whatever the lengths. */
+VECTOR_API size_t vector_decode_q4_workspace_bytes(const vector_shape* shape);
+
+/*
+ * vector_decode_attn (mode 0) over the paged cache: each sequence attends to its own ret_len and apx_len rows, read on the device, so that a captured call
+ * follows them.  A sequence with no rows gives zeros; an entry of a table outside its pool stands for rows that are not there.
+ * q: device [U][g][d] of shape->dtype; W: device [L * Hkv][d][d]; out: device [U][g][d] of out_dtype.
+ */
+VECTOR_API vector_status vector_decode_attn_q4(const vector_shape* shape, const void* q, const vector_q4_cache* cache, const void* W,
+                                               void* out, int32_t out_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Allocation-free variant of vector_decode_attn (the paper has no counterpart:
  * this entry point exists for the integration, not for the method).
  *

@@ -14,5 +14,7 @@ from .binding import (  # noqa: F401
     vector_layer_workspace_bytes, vector_layer_scores, vector_residual_layer, vector_route_layer, vector_compact_layer,
     vector_decode_attn_layer,
     vector_r2_global, vector_r2_global_workspace_bytes, R2_FIELDS, vector_sync_check,
+    Q4Cache, VECTOR_PAGE_ROWS, vector_q4_tile_bytes, alloc_q4_cache, vector_block_tables, vector_compact_q4, vector_append_q4, vector_read_q4,
+    vector_decode_q4_workspace_bytes, vector_decode_attn_q4,
     vector_device_fault, vector_kernel_launches, vector_decode_attn_static, vector_decode_scratch_bytes, VECTOR_STATIC_SCRATCH_BYTES,
 )

@@ -65,6 +65,7 @@ class _Cache(ctypes.Structure):
 _pack_shape = struct.Struct("8ifif").pack
 _pack_budget = struct.Struct("7q").pack
 _pack_cache = struct.Struct("5P4q").pack
+_pack_q4_cache = struct.Struct("8P2q2i").pack
 
 
 @dataclass
@@ -138,6 +139,28 @@ class Cache:
                            self.ret_k.shape[1], self.apx_k.shape[1], self.n_ret, self.n_apx)
 
 
+VECTOR_PAGE_ROWS = 64
+
+
+@dataclass
+class Q4Cache:
+    """Device buffers of the 4-bit paged cache: pools of pages, and the tables and lengths of the sequences of a batch."""
+    ret_pages: torch.Tensor  # [n_ret_pages][L * Hkv][2 * tile] uint8: 64 rows of keys, then of values
+    apx_pages: torch.Tensor  # [n_apx_pages][L * Hkv][tile] uint8
+    ret_table: torch.Tensor  # [batch][width] int32
+    apx_table: torch.Tensor  # [batch][width] int32
+    ret_len: torch.Tensor    # [batch] int32, rows of each sequence
+    apx_len: torch.Tensor    # [batch] int32
+    ret_pos: torch.Tensor | None = None      # [n_ret_pages][L * Hkv][64] int32
+    apx_pos: torch.Tensor | None = None      # [n_apx_pages][L * Hkv][64] int32, needed where rope is on
+
+    def _p(self) -> bytes:
+        return _pack_q4_cache(self.ret_pages.data_ptr(), self.apx_pages.data_ptr(), self.ret_table.data_ptr(), self.apx_table.data_ptr(),
+                              self.ret_len.data_ptr(), self.apx_len.data_ptr(), 0 if self.ret_pos is None else self.ret_pos.data_ptr(),
+                              0 if self.apx_pos is None else self.apx_pos.data_ptr(), self.ret_pages.shape[0], self.apx_pages.shape[0],
+                              self.ret_table.shape[1], self.apx_table.shape[1])
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -189,6 +212,17 @@ def load_library() -> ctypes.CDLL:
     lib.vector_r2_global_workspace_bytes.argtypes = [SP, I64]
     lib.vector_r2_global.argtypes = [SP, P, P, P, I64, P, P, SZ, P]
     lib.vector_r2_global.restype = ctypes.c_int
+    lib.vector_q4_tile_bytes.restype = SZ
+    lib.vector_q4_tile_bytes.argtypes = [SP]
+    lib.vector_block_tables.argtypes = [I32, P, P, I32, P, I32, P, I32, P, P, P, P, P, P, I64, P]
+    lib.vector_compact_q4.argtypes = [SP, BP, P, P, P, P, CP, P, P, P]
+    lib.vector_append_q4.argtypes = [SP, CP, P, P, P, P, I64, P, P]
+    lib.vector_read_q4.argtypes = [SP, CP, P, I64, P, P, P, I64, P, P]
+    lib.vector_decode_q4_workspace_bytes.restype = SZ
+    lib.vector_decode_q4_workspace_bytes.argtypes = [SP]
+    lib.vector_decode_attn_q4.argtypes = [SP, P, CP, P, P, I32, P, SZ, P]
+    for name in ("vector_block_tables", "vector_compact_q4", "vector_append_q4", "vector_read_q4", "vector_decode_attn_q4"):
+        getattr(lib, name).restype = ctypes.c_int
     lib.vector_sync_check.argtypes = [P]
     lib.vector_sync_check.restype = ctypes.c_int
     for name in ("vector_layer_scores", "vector_residual_layer", "vector_route_layer", "vector_compact_layer",
@@ -554,6 +588,110 @@ def vector_decode_attn_layer(shape: Shape, q, cache: Cache, W_layer, out, ws=Non
                                                  c, _dev(W_layer, shape.torch_dtype, "W_layer"),
                                                  _dev(out, None, "out"), out_dt, wp, wn, _stream(stream))
     _check(rc, "vector_decode_attn_layer")
+
+
+# ---- the mixed cache in 4 bits and pages
+def _sized(t, dtype, n: int, name: str):
+    """A tensor of n elements at least, or None where n is 0."""
+    if t is None or not n:
+        if n:
+            raise ValueError(f"{name} is missing")
+        return None
+    p = _dev(t, dtype, name)
+    if t.numel() < n:
+        raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
+    return p
+
+
+def _q4(shape: Shape, cache: Q4Cache, attends: bool = False) -> bytes:
+    """The cache's struct, its tensors checked; tables and lengths where the call reads them."""
+    tile, LH = vector_q4_tile_bytes(shape), shape.n_layers * shape.n_kv_heads
+    for t, n, name in ((cache.ret_pages, 2 * tile, "ret_pages"), (cache.apx_pages, tile, "apx_pages")):
+        _dev(t, torch.uint8, name)
+        if t.dim() != 3 or tuple(t.shape[1:]) != (LH, n):
+            raise ValueError(f"{name} must be [pages][{LH}][{n}], got {tuple(t.shape)}")
+    for t, pages, name in ((cache.ret_pos, cache.ret_pages, "ret_pos"), (cache.apx_pos, cache.apx_pages, "apx_pos")):
+        if t is not None:
+            _sized(t, torch.int32, pages.shape[0] * LH * VECTOR_PAGE_ROWS, name)
+    if attends:
+        for t, n, name in ((cache.ret_table, cache.ret_len, "ret"), (cache.apx_table, cache.apx_len, "apx")):
+            _dev(t, torch.int32, name + "_table")
+            if t.dim() != 2 or t.shape[0] < shape.batch:
+                raise ValueError(f"{name}_table must be [{shape.batch}][width], got {tuple(t.shape)}")
+            _sized(n, torch.int32, shape.batch, name + "_len")
+    return cache._p()
+
+
+def vector_q4_tile_bytes(shape: Shape) -> int:
+    """Bytes of a page's 64 rows of one (layer, KV head)."""
+    return int(load_library().vector_q4_tile_bytes(shape._p()))
+
+
+def alloc_q4_cache(shape: Shape, ret_pages: int, apx_pages: int, ret_width: int, apx_width: int, positions: bool = True, device="cuda") -> Q4Cache:
+    """Pools of so many pages, and tables of so many pages a sequence; no sequence has any rows."""
+    tile, LH, B = vector_q4_tile_bytes(shape), shape.n_layers * shape.n_kv_heads, shape.batch
+    ints = lambda *size: torch.empty(*size, dtype=torch.int32, device=device)  # noqa: E731
+    return Q4Cache(torch.empty(ret_pages, LH, 2 * tile, dtype=torch.uint8, device=device), torch.empty(apx_pages, LH, tile, dtype=torch.uint8, device=device),
+                   ints(B, ret_width).fill_(-1), ints(B, apx_width).fill_(-1), ints(B).zero_(), ints(B).zero_(),
+                   ints(ret_pages, LH, VECTOR_PAGE_ROWS) if positions else None, ints(apx_pages, LH, VECTOR_PAGE_ROWS) if positions else None)
+
+
+def vector_block_tables(lengths, added, page_rows: int, table, free_pages, n_free, new_lengths, new_n_free, first_row, row_start, slots=None, stream=None):
+    """Tables, lengths and slots after request b changed by added[b] rows; new_lengths may be lengths and new_n_free n_free."""
+    if table.dim() != 2:
+        raise ValueError("table must be [batch][width]")
+    B, i32 = table.shape[0], torch.int32
+    n_slots = 0 if slots is None else slots.numel()
+    rc = load_library().vector_block_tables(B, _sized(lengths, i32, B, "lengths"), _sized(added, i32, B, "added"), page_rows, _dev(table, i32, "table"),
+                                            table.shape[1], _dev(free_pages, i32, "free_pages"), free_pages.numel(), _sized(n_free, i32, 1, "n_free"),
+                                            _sized(new_lengths, i32, B, "new_lengths"), _sized(new_n_free, i32, 1, "new_n_free"),
+                                            _sized(first_row, i32, B, "first_row"), _sized(row_start, i32, B + 1, "row_start"),
+                                            _sized(slots, i32, n_slots, "slots"), n_slots, _stream(stream))
+    _check(rc, "vector_block_tables")
+
+
+def vector_compact_q4(shape: Shape, budget: Budget, K, V, ret_idx, apx_idx, cache: Q4Cache, ret_slots, apx_slots, stream=None):
+    U, B, d = shape.units, shape.batch, shape.head_dim
+    rc = load_library().vector_compact_q4(shape._p(), budget._p(), _sized(K, shape.torch_dtype, U * budget.n_tokens * d, "K"),
+                                          _sized(V, shape.torch_dtype, U * budget.n_tokens * d, "V"),
+                                          _sized(ret_idx, torch.int32, U * budget.n_ret, "ret_idx"), _sized(apx_idx, torch.int32, U * budget.n_apx, "apx_idx"),
+                                          _q4(shape, cache), _sized(ret_slots, torch.int32, B * budget.n_ret, "ret_slots"),
+                                          _sized(apx_slots, torch.int32, B * budget.n_apx, "apx_slots"), _stream(stream))
+    _check(rc, "vector_compact_q4")
+
+
+def vector_append_q4(shape: Shape, cache: Q4Cache, k_new, v_new, row_start, slots, pos=None, stream=None):
+    """k_new, v_new [U][d]: the rows of sequence b go to slots[row_start[b]], or to slots[b] where row_start is None."""
+    B, n = shape.batch, shape.units * shape.head_dim
+    rc = load_library().vector_append_q4(shape._p(), _q4(shape, cache), _sized(k_new, shape.torch_dtype, n, "k_new"), _sized(v_new, shape.torch_dtype, n, "v_new"),
+                                         None if row_start is None else _sized(row_start, torch.int32, B + 1, "row_start"),
+                                         _dev(slots, torch.int32, "slots"), slots.numel(), None if pos is None else _sized(pos, torch.int32, B, "pos"), _stream(stream))
+    _check(rc, "vector_append_q4")
+
+
+def vector_read_q4(shape: Shape, cache: Q4Cache, ret_slots=None, ret_k=None, ret_v=None, apx_slots=None, apx_k=None, stream=None):
+    """Rows of slots [batch][n] as values [U][n][d]: retained ones to ret_k and ret_v, key-only ones to apx_k."""
+    U, B, d, dt = shape.units, shape.batch, shape.head_dim, shape.torch_dtype
+    n_ret, n_apx = (0 if t is None else t.numel() // B for t in (ret_slots, apx_slots))
+    rc = load_library().vector_read_q4(shape._p(), _q4(shape, cache), _sized(ret_slots, torch.int32, B * n_ret, "ret_slots"), n_ret,
+                                       _sized(ret_k, dt, U * n_ret * d, "ret_k"), _sized(ret_v, dt, U * n_ret * d, "ret_v"),
+                                       _sized(apx_slots, torch.int32, B * n_apx, "apx_slots"), n_apx, _sized(apx_k, dt, U * n_apx * d, "apx_k"), _stream(stream))
+    _check(rc, "vector_read_q4")
+
+
+def vector_decode_q4_workspace_bytes(shape: Shape) -> int:
+    return int(load_library().vector_decode_q4_workspace_bytes(shape._p()))
+
+
+def vector_decode_attn_q4(shape: Shape, q, cache: Q4Cache, W, out, ws=None, stream=None):
+    wp, wn = _ws(ws)
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out must be fp32 or bf16")
+    n, d = shape.units * shape.group * shape.head_dim, shape.head_dim
+    rc = load_library().vector_decode_attn_q4(shape._p(), _sized(q, shape.torch_dtype, n, "q"), _q4(shape, cache, attends=True),
+                                              _sized(W, shape.torch_dtype, shape.n_layers * shape.n_kv_heads * d * d, "W"), _sized(out, out.dtype, n, "out"),
+                                              VECTOR_BF16 if out.dtype == torch.bfloat16 else VECTOR_F32, wp, wn, _stream(stream))
+    _check(rc, "vector_decode_attn_q4")
 
 
 VECTOR_STATIC_SCRATCH_BYTES = 16 << 20

@@ -1,0 +1,218 @@
+// Page tables, lengths and slots of a batch of requests after some grew, shrank or ended (vector_block_tables), from nothing but the
+// requests' lengths and changes.  Everything is a prefix sum over the requests: pages released (pushed on the stack of free pages in the
+// requests' order), pages wanted (popped in that order) and rows added.  So no answer depends on the order in which threads run.
+//
+// What bounds a step of a batch is latency: one block does all of it, a thread a request, and writes the few slots too.  An
+// admission has millions of slots, 4 bytes each: a second kernel writes them, over all multiprocessors.
+#include "common.cuh"
+#include "internal.h"
+
+namespace vec {
+namespace bt {
+
+constexpr int THREADS = 1024, SLOT_THREADS = 256, SLOTS_PER_WARP = 128;
+constexpr int FEW_SLOTS = 4096;                 // slots that the first kernel writes itself, of at most THREADS requests
+
+struct Args {
+    const int32_t *lengths, *added;
+    int32_t *new_lengths, *table, *stack, *new_n_free, *first_row, *row_start, *slots;
+    const int32_t* n_free;
+    int64_t n_slots;
+    int32_t batch, page_rows, width, cap_free;
+};
+
+// A request's change in pages; rows: after the change, if there are pages enough.  width * page_rows is below 2^31.
+struct Change { int64_t old_rows, rows; int have, want; };
+__device__ __forceinline__ Change change_of(const Args& a, int b) {
+    Change c;
+    const int64_t most = (int64_t)a.width * a.page_rows;
+    c.old_rows = min((int64_t)max(a.lengths[b], 0), most);
+    c.rows = max(c.old_rows + a.added[b], (int64_t)0);
+    c.have = (int)(((uint32_t)c.old_rows + (uint32_t)a.page_rows - 1) / (uint32_t)a.page_rows);
+    c.want = (int)(((uint32_t)min(c.rows, most) + (uint32_t)a.page_rows - 1) / (uint32_t)a.page_rows);
+    return c;
+}
+
+// Sum of x over the threads before this one; `total` over all.  All threads of the block.
+__device__ __forceinline__ int64_t scan(int64_t x, int64_t* warps, int64_t& total) {
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
+    int64_t s = x;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += y;
+    }
+    __syncthreads();                                             // the sums of the scan before have been read
+    if (lane == 31) warps[wid] = s;
+    __syncthreads();
+    int64_t w = warps[lane];                                     // THREADS / 32 = 32 warps
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(0xffffffffu, w, o);
+        if (lane >= o) w += y;
+    }
+    total = __shfl_sync(0xffffffffu, w, 31);
+    const int64_t before = __shfl_sync(0xffffffffu, w, max(wid - 1, 0));
+    return s - x + (wid ? before : 0);
+}
+
+// f(i, row, at) for i in [0, n) of every lane's own n, row and at: a lane alone while they are few, all lanes together for the long ones.
+template <typename F>
+__device__ __forceinline__ void each(int n, int32_t* row, int64_t at, F f) {
+    constexpr int FEW = 4;
+    if (n <= FEW)
+        for (int i = 0; i < n; ++i) f(i, row, at);
+    for (unsigned big = __ballot_sync(0xffffffffu, n > FEW); big; big &= big - 1) {
+        const int src = __ffs(big) - 1;
+        const int m = __shfl_sync(0xffffffffu, n, src);
+        int32_t* r = (int32_t*)__shfl_sync(0xffffffffu, (unsigned long long)row, src);
+        const int64_t p = __shfl_sync(0xffffffffu, at, src);
+        for (int i = threadIdx.x & 31; i < m; i += 32) f(i, r, p);
+    }
+}
+
+// The request that row k of the added rows belongs to: the last b in [lo, hi) with start[b] <= k.
+__device__ __forceinline__ int request_of(const int32_t* start, int lo, int hi, int64_t k) {
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (start[mid] <= k) lo = mid;
+        else hi = mid;
+    }
+    return lo;
+}
+// Slot of the k-th added row, which is one of request b's.
+__device__ __forceinline__ int32_t slot_of(const Args& a, int b, int64_t start, int64_t k) {
+    const int64_t row = a.first_row[b] + (k - start);
+    if (row >= a.new_lengths[b]) return -1;                      // no page was left for it
+    const uint32_t page = (uint32_t)row / (uint32_t)a.page_rows;
+    const int64_t at = a.table[(size_t)b * a.width + page];
+    const int64_t slot = at * a.page_rows + (int64_t)((uint32_t)row - page * (uint32_t)a.page_rows);
+    return at < 0 || slot > 0x7fffffffLL ? -1 : (int32_t)slot;
+}
+
+__global__ void __launch_bounds__(THREADS)
+block_tables_plan(Args a, int with_slots) {
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    __shared__ int64_t warps[32];
+    __shared__ int32_t starts[THREADS + 1];
+    const int t = threadIdx.x;
+    int64_t height = min(max((int64_t)a.n_free[0], (int64_t)0), (int64_t)a.cap_free);
+
+    // ---- released pages go on the stack, a request's in the order of its table
+    int64_t total = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
+        const int b = b0 + t;
+        Change c = {};
+        if (b < a.batch) c = change_of(a, b);
+        const int back = max(c.have - c.want, 0);
+        if (!__syncthreads_or(back > 0)) continue;
+        const int64_t at = height + scan(back, warps, total);
+        each(back, a.table + (size_t)b * a.width + c.want, at, [&](int i, int32_t* row, int64_t p) {
+            if (p + i < a.cap_free) a.stack[p + i] = row[i];
+        });
+        height = min(height + total, (int64_t)a.cap_free);
+    }
+    __syncthreads();
+    // ---- wanted pages come off it, as far as they go; lengths and the rows' starts
+    int64_t needed = 0, added = 0;
+    for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
+        const int b = b0 + t;
+        Change c = {};
+        int grow = 0;
+        if (b < a.batch) { c = change_of(a, b); grow = a.added[b]; }
+        const int need = max(c.want - c.have, 0);
+        const int64_t start = added + scan(max(grow, 0), warps, total);
+        added += total;
+        int64_t before = needed;
+        if (__syncthreads_or(need > 0)) {
+            before += scan(need, warps, total);
+            needed += total;
+        }
+        const int got = (int)min((int64_t)need, max(height - before, (int64_t)0));
+        each(got, a.table + (size_t)b * a.width + c.have, height - 1 - before, [&](int i, int32_t* row, int64_t p) { row[i] = a.stack[p - i]; });
+        if (b < a.batch) {
+            const int32_t s = (int32_t)min(start, (int64_t)0x7fffffff);
+            a.first_row[b] = (int32_t)c.old_rows;
+            a.row_start[b] = s;
+            a.new_lengths[b] = (int32_t)(grow > 0 ? min(c.rows, (int64_t)(c.have + got) * a.page_rows) : c.rows);
+            if (with_slots) starts[t] = s;
+        }
+    }
+    if (t == 0) {
+        a.row_start[a.batch] = (int32_t)min(added, (int64_t)0x7fffffff);
+        a.new_n_free[0] = (int32_t)(height - min(needed, height));
+    }
+    if (!with_slots) return;
+    __syncthreads();
+    for (int64_t k = t; k < a.n_slots; k += THREADS) {
+        int32_t slot = -1;
+        if (k < added) {
+            const int b = request_of(starts, 0, a.batch, k);
+            slot = slot_of(a, b, starts[b], k);
+        }
+        a.slots[k] = slot;
+    }
+}
+
+// The slots of all added rows, SLOTS_PER_WARP neighbours a warp, four a lane; -1 behind the last.
+__global__ void __launch_bounds__(SLOT_THREADS)
+block_tables_slots(Args a) {
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    const int lane = threadIdx.x & 31;
+    const int64_t k0 = ((int64_t)blockIdx.x * (SLOT_THREADS / 32) + (threadIdx.x >> 5)) * SLOTS_PER_WARP;
+    if (k0 >= a.n_slots) return;
+    const int64_t added = a.row_start[a.batch];
+    int32_t got[4] = {-1, -1, -1, -1};
+    const int64_t k = k0 + 4 * lane;
+    if (k0 < added) {
+        // the warp looks for the request of its first row: 32 places at a time
+        int lo = 0, hi = a.batch;
+        while (hi - lo > 1) {
+            const int step = (hi - lo + 31) / 32, at = lo + lane * step;
+            const unsigned under = __ballot_sync(0xffffffffu, at < hi && a.row_start[min(at, a.batch)] <= k0);
+            const int last = 31 - __clz(under);                  // lane 0 looks at lo, which is not beyond the row
+            hi = min(lo + (last + 1) * step, hi);
+            lo += last * step;
+        }
+        int b = lo;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (k + i >= added) break;
+            if (a.row_start[b + 1] <= k + i) b = request_of(a.row_start, b + 1, a.batch, k + i);
+            got[i] = slot_of(a, b, a.row_start[b], k + i);
+        }
+    }
+    if (k + 4 <= a.n_slots && ((uintptr_t)a.slots & 15) == 0) {
+        *reinterpret_cast<int4*>(a.slots + k) = make_int4(got[0], got[1], got[2], got[3]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (k + i < a.n_slots) a.slots[k + i] = got[i];
+    }
+}
+
+}  // namespace bt
+}  // namespace vec
+
+using namespace vec;
+
+extern "C" vector_status vector_block_tables(int32_t batch, const int32_t* lengths, const int32_t* added, int32_t page_rows, int32_t* table,
+                                             int32_t width, int32_t* free_pages, int32_t cap_free, const int32_t* n_free, int32_t* new_lengths,
+                                             int32_t* new_n_free, int32_t* first_row, int32_t* row_start, int32_t* slots, int64_t n_slots,
+                                             void* stream) {
+    if (!lengths || !added || !table || !free_pages || !n_free || !new_lengths || !new_n_free || !first_row || !row_start) return VECTOR_ERR_NULL;
+    if (n_slots > 0 && !slots) return VECTOR_ERR_NULL;
+    if (batch < 1 || batch > 65535 || page_rows < 1 || width < 1 || cap_free < 0 || n_slots < 0 || n_slots > 0x7fffffffLL ||
+        (int64_t)width * page_rows > 0x7fffffffLL)
+        return VECTOR_ERR_SHAPE;
+    const bt::Args a = {lengths, added, new_lengths, table, free_pages, new_n_free, first_row, row_start, slots, n_free, n_slots, batch, page_rows, width, cap_free};
+    const bool few = n_slots <= bt::FEW_SLOTS && batch <= bt::THREADS;
+    cudaStream_t st = (cudaStream_t)stream;
+    VEC_CUDA_CHECK(launch_maybe_dependent(true, bt::block_tables_plan, dim3(1), dim3(bt::THREADS), 0, st, a, few ? 1 : 0));
+    if (few || n_slots == 0) return VECTOR_OK;
+    const int64_t per_block = (int64_t)bt::SLOT_THREADS / 32 * bt::SLOTS_PER_WARP;
+    VEC_CUDA_CHECK(launch_maybe_dependent(true, bt::block_tables_slots, dim3((unsigned)((n_slots + per_block - 1) / per_block)), dim3(bt::SLOT_THREADS), 0, st, a));
+    return VECTOR_OK;
+}

@@ -36,6 +36,9 @@ vector_status check_shape(const vector_shape* s, Dims* out);
 // Checks internal consistency of tier sizes (the identities of the planner).
 vector_status check_budget(const vector_budget* b, int window);
 
+// Checks the pools of a 4-bit cache (not its tables and lengths, which attention alone reads).
+vector_status check_q4_cache(const vector_q4_cache* c);
+
 void set_last_cuda_error(int e);
 // Adds one to the process-wide count of kernels launched by the library (vector_kernel_launches).
 void count_launch();
