@@ -103,42 +103,72 @@ __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
 }
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
-// Where a worker is in the sequence of tiles.
-struct Walk {
-    int b, lh, t, n_ret, n_apx;                 // sequence, (layer, KV head), tile of the unit, rows
+// A worker's way through the sequence of tiles, as runs: tiles of one tier of one unit.
+struct Runs {
+    int64_t left;                               // cost up to the end of the worker's range
+    int b, lh, n_ret, n_apx;                    // sequence, (layer, KV head), rows
+    int apx, p, count;                          // the run: tier, first tile of it, tiles
     __device__ __forceinline__ void enter(const Cache& c) {
         n_ret = rows_of(c.ret_len, b, c.ret_width);
         n_apx = rows_of(c.apx_len, b, c.apx_width);
     }
-    __device__ __forceinline__ int tiles() const { return tiles_of(n_ret) + tiles_of(n_apx); }
-    __device__ __forceinline__ void settle(const Cache& c, const int64_t* prefix) {       // t may be behind the unit's last tile
-        if (t < tiles()) return;
-        t = 0;
-        if (++lh < c.LH) return;
-        lh = 0;
-        do ++b; while (b < c.batch && prefix[b + 1] == prefix[b]);
-        if (b < c.batch) enter(c);
+    // The run that begins with tile t of the present unit, or of the next one if there is none; no tiles at the end of the range.
+    __device__ __forceinline__ void run(const Cache& c, const int64_t* prefix, int t) {
+        int nr = tiles_of(n_ret);
+        if (t >= nr + tiles_of(n_apx)) {
+            t = 0;
+            if (++lh == c.LH) {
+                lh = 0;
+                do ++b; while (b < c.batch && prefix[b + 1] == prefix[b]);
+                if (b < c.batch) { enter(c); nr = tiles_of(n_ret); }
+            }
+        }
+        apx = t >= nr;
+        p = apx ? t - nr : t;
+        const int64_t in_range = apx ? (left + COST_APX - 1) / COST_APX : (left + COST_RET - 1) / COST_RET;
+        count = b < c.batch ? (int)max(min((int64_t)((apx ? tiles_of(n_apx) : nr) - p), in_range), (int64_t)0) : 0;
+        left -= (int64_t)count * (apx ? COST_APX : COST_RET);
     }
-    // The first tile that begins at cost x or later.
-    __device__ __forceinline__ void find(const Cache& c, const int64_t* prefix, int64_t x) {
-        int lo = 0, hi = c.batch + 1;           // the last b with prefix[b] <= x
+    __device__ __forceinline__ void next(const Cache& c, const int64_t* prefix) { run(c, prefix, p + count + (apx ? tiles_of(n_ret) : 0)); }
+    // The first run of the costs [x, end).
+    __device__ __forceinline__ void find(const Cache& c, const int64_t* prefix, int64_t x, int64_t end) {
+        int lo = 0, hi = c.batch;               // the last b with prefix[b] <= x
         while (hi - lo > 1) {
             const int mid = (lo + hi) >> 1;
             if (prefix[mid] <= x) lo = mid;
             else hi = mid;
         }
-        b = lo; lh = 0; t = 0; n_ret = 0; n_apx = 0;
-        if (b >= c.batch) return;
+        b = lo;
         enter(c);
-        const int64_t r = x - prefix[b], unit = (prefix[b + 1] - prefix[b]) / c.LH;
-        lh = (int)(r / unit);
-        t = tile_from(r - lh * unit, tiles_of(n_ret));
-        settle(c, prefix);
+        const int64_t unit = (prefix[b + 1] - prefix[b]) / c.LH;
+        lh = (int)((x - prefix[b]) / unit);
+        const int64_t r = x - prefix[b] - lh * unit;
+        const int nr = tiles_of(n_ret), t = tile_from(r, nr);
+        left = end - x - ((t < nr ? (int64_t)COST_RET * t : (int64_t)COST_RET * nr + (int64_t)COST_APX * (t - nr)) - r);
+        run(c, prefix, t);
     }
 };
 
 // What a slot holds, for its consumer: unit, rows that are there, tier, whether it is the unit's first tile.
 struct Tile { int unit, rows, apx, first; };
+
+// N neighbouring numbers at a multiple of 16 bytes.
+template <int N> __device__ __forceinline__ void load_run(const float* p, float* x) {
+#pragma unroll
+    for (int i = 0; i < N / 4; ++i) {
+        const float4 v = reinterpret_cast<const float4*>(p)[i];
+        x[4 * i] = v.x; x[4 * i + 1] = v.y; x[4 * i + 2] = v.z; x[4 * i + 3] = v.w;
+    }
+}
+template <int N> __device__ __forceinline__ void load_run(const __nv_bfloat16* p, float* x) {
+#pragma unroll
+    for (int i = 0; i < N / 8; ++i) {
+        const uint4 v = reinterpret_cast<const uint4*>(p)[i];
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { x[8 * i + 2 * j] = __uint_as_float(w[j] << 16); x[8 * i + 2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u); }
+    }
+}
 
 template <typename T, int D, bool ROPE, bool EXACT>
 __global__ void __launch_bounds__(Cfg<T, D, ROPE, EXACT>::THREADS, 1)
@@ -201,38 +231,45 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     unsigned char* ring = smem + wid * SLOTS * C::SLOT_BYTES;
     const uint64_t policy = tma::policy_evict_first();
 
-    // ---- the producing side: `next` walks SLOTS tiles ahead
-    Walk next, end;
-    end.find(c, prefix, deal.begin(worker + 1));
-    next.find(c, prefix, deal.begin(worker));
-    auto more = [&] { return next.b != end.b || next.lh != end.lh || next.t != end.t; };
+    // ---- the producing side, SLOTS tiles ahead: `run` is where it is, `k` tiles of it are on their way, and lane l has the page of tile l of 32
+    Runs run;
+    run.find(c, prefix, deal.begin(worker), deal.begin(worker + 1));
+    int k = 0, page = -1;
+    size_t row_at = 0;
     auto issue = [&](int s) {
-        const int nr = tiles_of(next.n_ret);
-        const bool apx = next.t >= nr;
-        const int p = apx ? next.t - nr : next.t;
-        const int64_t page = apx ? c.apx_table[(size_t)next.b * c.apx_width + p] : c.ret_table[(size_t)next.b * c.ret_width + p];
-        const bool there = page >= 0 && page < (apx ? c.n_apx_pages : c.n_ret_pages);
+        if ((k & 31) == 0) {
+            row_at = run.apx ? (size_t)run.b * c.apx_width + run.p : (size_t)run.b * c.ret_width + run.p;
+            if (k + lane < run.count) page = (run.apx ? c.apx_table : c.ret_table)[row_at + k + lane];
+        }
+        const int at = __shfl_sync(0xffffffffu, page, k & 31);
         if (lane == 0) {
-            tiles[wid][s] = Tile{next.b * c.LH + next.lh, there ? min((apx ? next.n_apx : next.n_ret) - p * q4::ROWS, (int)q4::ROWS) : 0, apx, next.t == 0};
-            const size_t at = (size_t)page * c.LH + next.lh;
+            const bool there = at >= 0 && at < (run.apx ? c.n_apx_pages : c.n_ret_pages);
+            const int p = run.p + k;
+            const size_t tile = (size_t)at * c.LH + run.lh;
+            tiles[wid][s] = Tile{run.b * c.LH + run.lh, there ? min((run.apx ? run.n_apx : run.n_ret) - p * q4::ROWS, (int)q4::ROWS) : 0, run.apx,
+                                 p == 0 && (!run.apx || run.n_ret == 0)};
+            uint64_t* bar = &full[wid][s];
+            unsigned char* to = ring + s * C::SLOT_BYTES;
             if (!there) {
-                tma::mbar_arrive(&full[wid][s]);
-            } else if (apx) {
-                tma::mbar_expect_tx(&full[wid][s], R::TILE + (ROPE ? 4 * q4::ROWS : 0));
-                tma::load_bulk_hint(ring + s * C::SLOT_BYTES, c.apx + at * R::TILE, R::TILE, &full[wid][s], policy);
-                if (ROPE) tma::load_bulk_hint(ring + s * C::SLOT_BYTES + C::POS_AT, c.apx_pos + at * q4::ROWS, 4 * q4::ROWS, &full[wid][s], policy);
+                tma::mbar_arrive(bar);
+            } else if (run.apx) {
+                tma::mbar_expect_tx(bar, R::TILE + (ROPE ? 4 * q4::ROWS : 0));
+                tma::load_bulk_hint(to, c.apx + tile * R::TILE, R::TILE, bar, policy);
+                if (ROPE) tma::load_bulk_hint(to + C::POS_AT, c.apx_pos + tile * q4::ROWS, 4 * q4::ROWS, bar, policy);
             } else {
-                tma::mbar_expect_tx(&full[wid][s], 2 * R::TILE);
-                tma::load_bulk_hint(ring + s * C::SLOT_BYTES, c.ret + at * 2 * R::TILE, 2 * R::TILE, &full[wid][s], policy);
+                tma::mbar_expect_tx(bar, 2 * R::TILE);
+                tma::load_bulk_hint(to, c.ret + tile * 2 * R::TILE, 2 * R::TILE, bar, policy);
             }
         }
-        ++next.t;
-        next.settle(c, prefix);
+        if (++k == run.count) {
+            run.next(c, prefix);
+            k = 0;
+        }
     };
     int ahead = 0;
 #pragma unroll
     for (int s = 0; s < SLOTS; ++s)
-        if (more()) { issue(s); ++ahead; }
+        if (run.count > 0) { issue(s); ++ahead; }
     __syncwarp();
 
     // ---- the consuming side
@@ -247,12 +284,14 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     clear();
     // The queries of a unit as B fragments: head gid, the channels of piece tig.  Scaled so that the largest lies in [2^7, 2^8).
     auto load_queries = [&](int unit) {
-        const T* row = q + ((size_t)unit * g + min(gid, g - 1)) * D;
+        const T* row = q + ((size_t)unit * g + min(gid, g - 1)) * D + tig * (D / 8);
         float x[2 * C::PAIRS];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) load_run<C::PAIRS>(row + h * (D / 2), &x[h * C::PAIRS]);
+        if (gid >= g) {
 #pragma unroll
-            for (int i = 0; i < C::PAIRS; ++i) x[h * C::PAIRS + i] = gid < g ? to_f32(row[h * (D / 2) + tig * (D / 8) + i]) : 0.f;
+            for (int i = 0; i < 2 * C::PAIRS; ++i) x[i] = 0.f;
+        }
         float most = 0.f;
 #pragma unroll
         for (int i = 0; i < 2 * C::PAIRS; ++i) most = fmaxf(most, fabsf(x[i]));
@@ -274,13 +313,13 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             }
         }
     };
-    // Rows 16 i + gid and 16 i + gid + 8 of a tile's 32 rows at `row0`, as A fragments; rows from `rows` on are zero.
-    auto load_rows = [&](const unsigned char* tile, int row0, int rows, uint32_t (&x)[2][2][C::PAIRS]) {
+    // Rows 16 i + gid and 16 i + gid + 8 of a tile's 32 rows at `row0`, as A fragments.
+    auto load_rows = [&](const unsigned char* tile, int row0, uint32_t (&x)[2][2][C::PAIRS]) {
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int r = 16 * i + 8 * h + gid, row = row0 + r;
+                const int row = row0 + 16 * i + 8 * h + gid;
                 uint32_t w[4];
                 if constexpr (D == 128) {
                     const uint4 v = *reinterpret_cast<const uint4*>(tile + row * R::CODES + tig * 16);
@@ -289,8 +328,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                     const uint2 v = *reinterpret_cast<const uint2*>(tile + row * R::CODES + tig * 8);
                     w[0] = v.x; w[1] = v.y;
                 }
-                uint32_t s = *reinterpret_cast<const uint16_t*>(tile + R::SCALES_AT + row * R::GROUPS + 2 * (D == 128 ? tig : tig >> 1));
-                if (r >= rows) s = 0;                                  // what lies there may be no number
+                const uint32_t s = *reinterpret_cast<const uint16_t*>(tile + R::SCALES_AT + row * R::GROUPS + 2 * (D == 128 ? tig : tig >> 1));
                 const uint32_t s2[2] = {(s & 0xffu) * 0x00800080u, (s >> 8) * 0x00800080u};
 #pragma unroll
                 for (int j = 0; j < D / 32; ++j) {
@@ -340,37 +378,49 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             apx = tile.apx;
             clear();
         }
-        const unsigned char* at = ring + s * C::SLOT_BYTES;
+        unsigned char* at = ring + s * C::SLOT_BYTES;
+        if (tile.rows < q4::ROWS) {            // what lies behind the last row may be no number: scales of zero
+            for (int i = tile.rows * R::GROUPS + lane; i < q4::ROWS * R::GROUPS; i += 32) {
+                at[R::SCALES_AT + i] = 0;
+                if (!tile.apx) at[R::TILE + R::SCALES_AT + i] = 0;
+            }
+            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+            __syncwarp();
+        }
 #pragma unroll 1
         for (int row0 = 0; row0 < tile.rows; row0 += 32) {
             const int rows = tile.rows - row0;
             uint32_t x[2][2][C::PAIRS];
-            load_rows(at, row0, rows, x);
+            load_rows(at, row0, x);
+            // ---- logits, in chains of two products (EXACT) or of half of them
             float S[2][4];
 #pragma unroll
-            for (int k = 0; k < 2; ++k) S[k][0] = S[k][1] = S[k][2] = S[k][3] = 0.f;
+            for (int i = 0; i < 2; ++i) S[i][0] = S[i][1] = S[i][2] = S[i][3] = 0.f;
+            constexpr int CHAIN = EXACT ? 2 : C::O_TILES / 2;
 #pragma unroll
-            for (int p = 0; p < C::Q_PARTS; ++p)
+            for (int p = C::Q_PARTS - 1; p >= 0; --p)
 #pragma unroll
-                for (int t = 0; t < C::O_TILES; ++t)
+                for (int t0 = 0; t0 < C::O_TILES; t0 += CHAIN)
 #pragma unroll
-                    for (int k = 0; k < 2; ++k)
-                        mma(S[k], x[k][0][2 * t], x[k][1][2 * t], x[k][0][2 * t + 1], x[k][1][2 * t + 1], qb[p][t][0], qb[p][t][1]);
+                    for (int i = 0; i < 2; ++i) {
+                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+                        for (int t = t0; t < t0 + CHAIN; ++t)
+                            mma(sum, x[i][0][2 * t], x[i][1][2 * t], x[i][0][2 * t + 1], x[i][1][2 * t + 1], qb[p][t][0], qb[p][t][1]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[k][e] *= fac[e & 1];
+                        for (int e = 0; e < 4; ++e) S[i][e] += sum[e];
+                    }
             if (rows < 32) {
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int i = 0; i < 2; ++i)
 #pragma unroll
                     for (int e = 0; e < 4; ++e)
-                        if (16 * k + 8 * (e >> 1) + gid >= rows) S[k][e] = -INFINITY;
+                        if (16 * i + 8 * (e >> 1) + gid >= rows) S[i][e] = -INFINITY;
             }
-            // ---- softmax against the reference m
+            // ---- softmax against the reference m (fac > 0)
             float top[2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) top[h] = fmaxf(fmaxf(S[0][h], S[0][2 + h]), fmaxf(S[1][h], S[1][2 + h]));
+            for (int h = 0; h < 2; ++h) top[h] = fmaxf(fmaxf(S[0][h], S[0][2 + h]), fmaxf(S[1][h], S[1][2 + h])) * fac[h];
             if (__any_sync(0xffffffffu, top[0] > m[0] + SLACK || top[1] > m[1] + SLACK)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -388,7 +438,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
-                    const float a = tc::ex2(S[k][2 * h] - m[0]), b = tc::ex2(S[k][2 * h + 1] - m[1]);
+                    const float a = tc::ex2(fmaf(S[k][2 * h], fac[0], -m[0])), b = tc::ex2(fmaf(S[k][2 * h + 1], fac[1], -m[1]));
                     const uint32_t hi = pack_h2(a, b);
                     ph[k][h] = transpose(hi);
                     if constexpr (EXACT) {
@@ -396,7 +446,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                         pl[k][h] = transpose(pack_h2(a - f.x, b - f.y));
                     }
                 }
-            if (!tile.apx) load_rows(at + R::TILE, row0, rows, x);
+            if (!tile.apx) load_rows(at + R::TILE, row0, x);
             uint32_t lo[2][2][ROPE && EXACT ? C::PAIRS : 1];           // second parts of keys turned back
             if constexpr (ROPE) {
                 if (tile.apx) {
@@ -472,130 +522,210 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         }
         __syncwarp();                                                  // every lane has read the slot
         --ahead;
-        if (more()) { issue(s); ++ahead; __syncwarp(); }
+        if (run.count > 0) { issue(s); ++ahead; __syncwarp(); }
     }
     leave_unit();
 }
 
 constexpr int MERGE_THREADS = 256;
+constexpr int FEW_PIECES = 4;        // records of a unit that every thread weighs for itself
+constexpr int MERGE_CHUNK = 64;      // records weighed at a time where there are more
+
+// The map's rows 16 w + gid and 16 w + gid + 8 as a thread holds them: channels 32 i + 8 tig .. + 7 of each.
+template <typename T, int D> struct MapRows;
+template <int D> struct MapRows<__nv_bfloat16, D> {
+    static constexpr int PARTS = 1;
+    uint4 w[2][D / 32];
+    __device__ __forceinline__ void load(const __nv_bfloat16* W, int tig) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i) w[h][i] = *reinterpret_cast<const uint4*>(W + h * 8 * D + 32 * i + 8 * tig);
+    }
+    __device__ __forceinline__ void pairs(int h, int i, uint32_t (&p)[4][1]) const { p[0][0] = w[h][i].x; p[1][0] = w[h][i].y; p[2][0] = w[h][i].z; p[3][0] = w[h][i].w; }
+};
+template <int D> struct MapRows<float, D> {
+    static constexpr int PARTS = 3;
+    float4 w[2][D / 16];
+    __device__ __forceinline__ void load(const float* W, int tig) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int i = 0; i < D / 16; ++i) w[h][i] = *reinterpret_cast<const float4*>(W + h * 8 * D + 32 * (i / 2) + 8 * tig + 4 * (i % 2));
+    }
+    __device__ __forceinline__ void pairs(int h, int i, uint32_t (&p)[4][3]) const {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float4 v = w[h][2 * i + j];
+            split_bf16<3>(v.x, v.y, p[2 * j]);
+            split_bf16<3>(v.z, v.w, p[2 * j + 1]);
+        }
+    }
+};
 
 // The records of a unit into its outputs.
 template <typename T, int D, typename TO>
 __global__ void __launch_bounds__(MERGE_THREADS)
 decode_q4_merge(const unsigned char* ws, Cache c, int g, int most_workers, const T* W, TO* __restrict__ out) {
     constexpr int NW = MERGE_THREADS / 32, ROWS_W = 16;
-    constexpr bool TENSOR = sizeof(T) == 2;
     __shared__ __align__(16) float val[8][D + 4], keys[8][D + 4];
-    __shared__ float ref[8], inv[8];
+    __shared__ float ref[8], inv[8], fac[2][8][MERGE_CHUNK];
     const int u = blockIdx.x, b = u / c.LH, lh = u - b * c.LH;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
-    // the map's rows of this warp, requested ahead of the wait: rows 16 wid + gid (+ 8), channels of lane tig
-    uint4 w[2][TENSOR ? D / 32 : 1];
-    if constexpr (TENSOR) {
-        if (wid < D / ROWS_W) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < D / 32; ++i)
-                    w[h][i] = *reinterpret_cast<const uint4*>(W + ((size_t)lh * D + ROWS_W * wid + 8 * h + gid) * D + 32 * i + 8 * tig);
-        }
-    }
+    MapRows<T, D> map;                   // requested ahead of the wait: the streaming kernel does not write it
+    if (wid < D / ROWS_W) map.load(W + ((size_t)lh * D + ROWS_W * wid + gid) * D, tig);
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     const int64_t* prefix = reinterpret_cast<const int64_t*>(ws);
     const float* records = reinterpret_cast<const float*>(ws + prefix_bytes(c.batch));
     const int heads = even_heads(g), tier = tier_floats(g, D), units = c.batch * c.LH;
     const int64_t p0 = prefix[b], p1 = prefix[b + 1], X = prefix[c.batch];
+    const int nr = tiles_of(rows_of(c.ret_len, b, c.ret_width)), na = tiles_of(rows_of(c.apx_len, b, c.apx_width));
     TO* o = out + (size_t)u * g * D;
     if (p0 == p1) {                                                   // nothing to attend to
         for (int e = threadIdx.x; e < g * D; e += MERGE_THREADS) store_out(o + e, 0.f);
         return;
     }
-    const int64_t cost = (p1 - p0) / c.LH, from = p0 + lh * cost;
+    const int64_t cost = (int64_t)COST_RET * nr + (int64_t)COST_APX * na, from = p0 + lh * cost;
     const Deal deal(X, most_workers);
-    const int nr = tiles_of(rows_of(c.ret_len, b, c.ret_width)), na = tiles_of(rows_of(c.apx_len, b, c.apx_width));
     const int w0 = deal.owner(from);
     int last = deal.owner(from + cost - 1);
     if (last > w0 && tile_from(deal.begin(last) - from, nr) >= nr + na) --last;       // its range begins within the unit's last tile
     const int pieces = last - w0 + 1;                                 // the unit's own record, then those of workers w0 + 1 ..
-    auto piece = [&](int i) { return records + (size_t)(i == 0 ? u : units + w0 + i) * 2 * tier; };
-    // ---- a warp a head: the largest reference, the sum of the weights
-    for (int h = wid; h < g; h += NW) {
-        float M = -INFINITY;
-        for (int i = lane; i < 2 * pieces; i += 32) M = fmaxf(M, piece(i >> 1)[(i & 1) * tier + 2 * h]);
-        M = warp_max(M);
-        float Lsum = 0.f;
-        for (int i = lane; i < 2 * pieces; i += 32) {
-            const float2 ml = *reinterpret_cast<const float2*>(piece(i >> 1) + (i & 1) * tier + 2 * h);
-            if (!(ml.x == -INFINITY)) Lsum = fmaf(exp2f(ml.x - M), ml.y, Lsum);
-        }
-        Lsum = warp_sum(Lsum);
-        if (lane == 0) { ref[h] = M; inv[h] = Lsum == 0.f ? 0.f : 1.f / Lsum; }
-    }
-    if (threadIdx.x < 8 && threadIdx.x >= g) { ref[threadIdx.x] = 0.f; inv[threadIdx.x] = 0.f; }
-    __syncthreads();
-    // ---- sums of values and of keys, four numbers (two rows of two heads) a thread
+    const float *own = records + (size_t)u * 2 * tier, *others = records + (size_t)(units + w0) * 2 * tier;
+    auto piece = [&](int i) { return i == 0 ? own : others + (size_t)i * 2 * tier; };
+    // Four numbers of a tier's sums are a thread's: rows `row` and `row` + 8 of O tile t, heads 2 hp and 2 hp + 1.
     const int quads = D / 16 * (heads / 2) * 8;
-    for (int e = threadIdx.x; e < 2 * quads; e += MERGE_THREADS) {
-        const int which = e >= quads, i = e - which * quads, row = i & 7, hp = (i >> 3) % (heads / 2), t = (i >> 3) / (heads / 2);
-        const float M0 = ref[2 * hp], M1 = ref[2 * hp + 1];
-        float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int k = 0; k < pieces; ++k) {
-            const float* p = piece(k) + which * tier;
-            const float4 ml = *reinterpret_cast<const float4*>(p + 4 * hp);
-            if (ml.x == -INFINITY && ml.z == -INFINITY) continue;
-            const float4 v = *reinterpret_cast<const float4*>(p + 2 * heads + 4 * i);
-            const float f0 = exp2f(ml.x - M0), f1 = exp2f(ml.z - M1);
-            a.x = fmaf(f0, v.x, a.x); a.y = fmaf(f1, v.y, a.y); a.z = fmaf(f0, v.z, a.z); a.w = fmaf(f1, v.w, a.w);
-        }
-        // rows `row` and `row` + 8 of O tile t: channel pairs 2 t and 2 t + 1 of piece row / 2
-        float (*to)[D + 4] = which ? keys : val;
+    auto put = [&](int which, int i, float4 a) {
+        const int row = i & 7, hp = (i >> 3) % (heads / 2), t = (i >> 3) / (heads / 2);
+        float (*to)[D + 4] = which ? keys : val;                      // channel pairs 2 t and 2 t + 1 of piece row / 2
         const int c0 = q4::Row<D>::channel_of(row / 2 * (D / 4) + 4 * t + row % 2), c1 = q4::Row<D>::channel_of(row / 2 * (D / 4) + 4 * t + 2 + row % 2);
         to[2 * hp][c0] = a.x; to[2 * hp + 1][c0] = a.y; to[2 * hp][c1] = a.z; to[2 * hp + 1][c1] = a.w;
-    }
-    __syncthreads();
-    // ---- the map
-    if constexpr (TENSOR) {
-        if (wid < D / ROWS_W) {
-            float acc[4] = {0.f, 0.f, 0.f, 0.f};
-            const int head = min(gid, heads - 1);
-            if (na > 0) {
+    };
+    auto add = [](float4& a, float f0, float f1, const float4& v) {
+        a.x = fmaf(f0, v.x, a.x); a.y = fmaf(f1, v.y, a.y); a.z = fmaf(f0, v.z, a.z); a.w = fmaf(f1, v.w, a.w);
+    };
+    if (pieces <= FEW_PIECES) {
+        // everything a thread needs is requested at once: the heads' references and sums of all records, and its numbers
+        for (int e = threadIdx.x; e < 2 * quads; e += MERGE_THREADS) {
+            const int which = e >= quads, i = e - which * quads, hp = (i >> 3) % (heads / 2);
+            float4 ml[FEW_PIECES][2], v[FEW_PIECES];
 #pragma unroll
-                for (int i = 0; i < D / 32; ++i) {
-                    const uint32_t r0[4] = {w[0][i].x, w[0][i].y, w[0][i].z, w[0][i].w}, r1[4] = {w[1][i].x, w[1][i].y, w[1][i].z, w[1][i].w};
-                    const float4 k0 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig]), k1 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig + 4]);
-                    uint32_t part[4][3];
-                    split_bf16<3>(k0.x, k0.y, part[0]); split_bf16<3>(k0.z, k0.w, part[1]);
-                    split_bf16<3>(k1.x, k1.y, part[2]); split_bf16<3>(k1.z, k1.w, part[3]);
-#pragma unroll
-                    for (int s = 0; s < 2; ++s)
-#pragma unroll
-                        for (int p = 2; p >= 0; --p)
-                            asm volatile(
-                                "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-                                : "+f"(acc[0]), "+f"(acc[1]), "+f"(acc[2]), "+f"(acc[3])
-                                : "r"(r0[2 * s]), "r"(r1[2 * s]), "r"(r0[2 * s + 1]), "r"(r1[2 * s + 1]), "r"(part[2 * s][p]), "r"(part[2 * s + 1][p]));
+            for (int k = 0; k < FEW_PIECES; ++k) {
+                ml[k][0] = ml[k][1] = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
+                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (k < pieces) {
+                    ml[k][0] = *reinterpret_cast<const float4*>(piece(k) + 4 * hp);
+                    ml[k][1] = *reinterpret_cast<const float4*>(piece(k) + tier + 4 * hp);
+                    v[k] = *reinterpret_cast<const float4*>(piece(k) + which * tier + 2 * heads + 4 * i);
                 }
             }
+            float M0 = -INFINITY, M1 = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int h = 2 * tig + (e & 1), ch = ROWS_W * wid + 8 * (e >> 1) + gid;
-                if (h < g) store_out(o + h * D + ch, (val[h][ch] + acc[e]) * inv[h]);
-            }
+            for (int k = 0; k < FEW_PIECES; ++k)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) { M0 = fmaxf(M0, ml[k][r].x); M1 = fmaxf(M1, ml[k][r].z); }
+            float L0 = 0.f, L1 = 0.f;
+            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+            for (int k = 0; k < FEW_PIECES; ++k)
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    if (ml[k][r].x == -INFINITY && ml[k][r].z == -INFINITY) continue;      // no such record, or an empty one: its numbers are not any
+                    const float f0 = exp2f(ml[k][r].x - M0), f1 = exp2f(ml[k][r].z - M1);
+                    L0 = fmaf(f0, ml[k][r].y, L0); L1 = fmaf(f1, ml[k][r].w, L1);
+                    if (r == which) add(a, f0, f1, v[k]);
+                }
+            put(which, i, a);
+            if (which == 0 && i < 8 * (heads / 2) && (i & 7) == 0) { inv[2 * hp] = L0 == 0.f ? 0.f : 1.f / L0; inv[2 * hp + 1] = L1 == 0.f ? 0.f : 1.f / L1; }
         }
     } else {
-        for (int r = wid; r < D; r += NW) {
-            float wr[D / 32];
+        // a warp a head: the largest reference, the sum of the weights
+        for (int h = wid; h < heads; h += NW) {
+            float M = -INFINITY;
+            for (int i = lane; i < 2 * pieces; i += 32) M = fmaxf(M, piece(i >> 1)[(i & 1) * tier + 2 * h]);
+            M = warp_max(M);
+            float sum = 0.f;
+            for (int i = lane; i < 2 * pieces; i += 32) {
+                const float2 ml = *reinterpret_cast<const float2*>(piece(i >> 1) + (i & 1) * tier + 2 * h);
+                if (!(ml.x == -INFINITY)) sum = fmaf(exp2f(ml.x - M), ml.y, sum);
+            }
+            sum = warp_sum(sum);
+            if (lane == 0) { ref[h] = M; inv[h] = sum == 0.f ? 0.f : 1.f / sum; }
+        }
+        float4 a[D / 64] = {};                                        // at most D / 64 rounds of numbers, with eight heads
+        for (int k0 = 0; k0 < pieces; k0 += MERGE_CHUNK) {
+            const int n = min(pieces - k0, MERGE_CHUNK);
+            __syncthreads();
+            for (int e = threadIdx.x; e < 2 * heads * n; e += MERGE_THREADS) {
+                const int k = e / (2 * heads), r = e - k * 2 * heads, h = r >> 1, which = r & 1;
+                const float m = piece(k0 + k)[which * tier + 2 * h];
+                fac[which][h][k] = m == -INFINITY ? 0.f : exp2f(m - ref[h]);
+            }
+            __syncthreads();
 #pragma unroll
-            for (int j = 0; j < D / 32; ++j) wr[j] = to_f32(W[((size_t)lh * D + r) * D + 32 * j + lane]);
-            for (int h = 0; h < g; ++h) {
-                float x = 0.f;
+            for (int j = 0; j < D / 64; ++j) {
+                const int e = threadIdx.x + j * MERGE_THREADS;
+                if (e >= 2 * quads) break;
+                const int which = e >= quads, i = e - which * quads, hp = (i >> 3) % (heads / 2);
+                const float *f0 = fac[which][2 * hp], *f1 = fac[which][2 * hp + 1];
+                constexpr int UN = 8;
+                for (int k = 0; k < n; k += UN) {
+                    float4 v[UN];
 #pragma unroll
-                for (int j = 0; j < D / 32; ++j) x = fmaf(wr[j], keys[h][32 * j + lane], x);
-                x = warp_sum(x);
-                if (lane == 0) store_out(o + h * D + r, (val[h][r] + x) * inv[h]);
+                    for (int z = 0; z < UN; ++z) {
+                        v[z] = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (k + z < n && (f0[k + z] != 0.f || f1[k + z] != 0.f))
+                            v[z] = *reinterpret_cast<const float4*>(piece(k0 + k + z) + which * tier + 2 * heads + 4 * i);
+                    }
+#pragma unroll
+                    for (int z = 0; z < UN; ++z)
+                        if (k + z < n) add(a[j], f0[k + z], f1[k + z], v[z]);
+                }
             }
         }
+#pragma unroll
+        for (int j = 0; j < D / 64; ++j) {
+            const int e = threadIdx.x + j * MERGE_THREADS;
+            if (e < 2 * quads) put(e >= quads, e >= quads ? e - quads : e, a[j]);
+        }
+    }
+    __syncthreads();
+    // ---- the map: its rows down, heads across; the key sums, and an fp32 map, in three bf16 parts, products down to 2^-16 of the largest
+    if (wid >= D / ROWS_W) return;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    if (na > 0) {
+        const int head = min(gid, heads - 1);
+#pragma unroll
+        for (int i = 0; i < D / 32; ++i) {
+            constexpr int P = MapRows<T, D>::PARTS;
+            uint32_t r0[4][P], r1[4][P], part[4][3];
+            map.pairs(0, i, r0);
+            map.pairs(1, i, r1);
+            const float4 k0 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig]), k1 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig + 4]);
+            split_bf16<3>(k0.x, k0.y, part[0]); split_bf16<3>(k0.z, k0.w, part[1]);
+            split_bf16<3>(k1.x, k1.y, part[2]); split_bf16<3>(k1.z, k1.w, part[3]);
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int p = 2; p >= 0; --p)
+#pragma unroll
+                    for (int r = P - 1; r >= 0; --r)
+                        if (p + r <= 2)
+                            asm volatile(
+                                "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                                : "+f"(sum[0]), "+f"(sum[1]), "+f"(sum[2]), "+f"(sum[3])
+                                : "r"(r0[2 * s][r]), "r"(r1[2 * s][r]), "r"(r0[2 * s + 1][r]), "r"(r1[2 * s + 1][r]), "r"(part[2 * s][p]), "r"(part[2 * s + 1][p]));
+#pragma unroll
+                for (int e = 0; e < 4; ++e) acc[e] += sum[e];
+            }
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const int h = 2 * tig + (e & 1), ch = ROWS_W * wid + 8 * (e >> 1) + gid;
+        if (h < g) store_out(o + h * D + ch, (val[h][ch] + acc[e]) * inv[h]);
     }
 }
 
