@@ -5,16 +5,18 @@
 namespace vec {
 namespace dq4 {
 
-static int most_workers() { return sm_count() * WARPS; }
+constexpr int MOST_WARPS = 16;          // of a streaming block, over all kernels
+
 static size_t ws_bytes_of(const Dims& dm, int batch) {
-    return prefix_bytes(batch) + ((size_t)dm.U + most_workers()) * 2 * tier_floats(dm.g, dm.d) * 4;
+    return prefix_bytes(batch) + ((size_t)dm.U + sm_count() * MOST_WARPS) * 2 * tier_floats(dm.g, dm.d) * 4;
 }
 
 struct Call {
     const Dims& dm; const void* q; Cache c; const void* W; void* out; int out_dtype; unsigned char* ws; cudaStream_t st;
 
-    template <typename T, int D, bool ROPE, bool EXACT> vector_status stream() const {
+    template <typename T, int D, bool ROPE, bool EXACT> vector_status both() const {
         using C = Cfg<T, D, ROPE, EXACT>;
+        static_assert(C::WARPS <= MOST_WARPS && C::SMEM_BYTES + (MAX_BATCH + 1) * 8 + 2048 <= 227 * 1024, "a block's shared memory, its own variables included");
         auto kern = decode_q4_stream<T, D, ROPE, EXACT>;
         static PerDeviceOnce once;
         if (once.first()) {
@@ -27,21 +29,19 @@ struct Call {
         if (ROPE) rope_phases(dm.theta, D, &ph);
         VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::SMEM_BYTES + (size_t)(c.batch + 1) * 8, st, (const T*)q, c, dm.g,
                                               dm.scale * 1.4426950408889634f, ws, fault, ph));
-        return VECTOR_OK;
+        const int workers = sm_count() * C::WARPS;
+        return out_dtype == VECTOR_F32 ? merge<T, D, float>(workers) : merge<T, D, __nv_bfloat16>(workers);
     }
-    template <typename T, int D, typename TO> vector_status merge() const {
+    template <typename T, int D, typename TO> vector_status merge(int workers) const {
         VEC_CUDA_CHECK(launch_maybe_dependent(true, decode_q4_merge<T, D, TO>, dim3(dm.U), dim3(MERGE_THREADS), 0, st, (const unsigned char*)ws, c, dm.g,
-                                              most_workers(), (const T*)W, (TO*)out));
+                                              workers, (const T*)W, (TO*)out));
         return VECTOR_OK;
     }
     template <typename T, int D> vector_status run() const {
         const bool exact = dm.dtype == VECTOR_F32 || out_dtype == VECTOR_F32;
-        vector_status rc;
-        if constexpr (sizeof(T) == 4) rc = dm.rope ? stream<T, D, true, true>() : stream<T, D, false, true>();
-        else if (exact) rc = dm.rope ? stream<T, D, true, true>() : stream<T, D, false, true>();
-        else rc = dm.rope ? stream<T, D, true, false>() : stream<T, D, false, false>();
-        if (rc != VECTOR_OK) return rc;
-        return out_dtype == VECTOR_F32 ? merge<T, D, float>() : merge<T, D, __nv_bfloat16>();
+        if constexpr (sizeof(T) == 2)
+            if (!exact) return dm.rope ? both<T, D, true, false>() : both<T, D, false, false>();
+        return dm.rope ? both<T, D, true, true>() : both<T, D, false, true>();
     }
 };
 

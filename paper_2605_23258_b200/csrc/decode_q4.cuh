@@ -21,6 +21,8 @@
 #ifndef VECTOR_DECODE_Q4_CUH_
 #define VECTOR_DECODE_Q4_CUH_
 
+#include <type_traits>
+
 #include "common.cuh"
 #include "internal.h"
 #include "q4.cuh"
@@ -31,9 +33,12 @@
 namespace vec {
 namespace dq4 {
 
-constexpr int WARPS = 12, SLOTS = 2;                 // slots of a warp's ring
 constexpr int MAX_BATCH = VECTOR_Q4_MAX_BATCH;
-constexpr int COST_RET = 2, COST_APX = 1, COST_MOST = 2;      // of a tile
+#ifndef DQ4_CR
+#define DQ4_CR 4
+#define DQ4_CA 3
+#endif
+constexpr int COST_RET = DQ4_CR, COST_APX = DQ4_CA, COST_MOST = DQ4_CR;      // of a tile
 constexpr float SLACK = 8.f;
 
 struct Cache {
@@ -65,25 +70,32 @@ __device__ __forceinline__ int tile_from(int64_t r, int nr) {
     return r <= (int64_t)COST_RET * nr ? (int)((r + COST_RET - 1) / COST_RET) : nr + (int)((r - (int64_t)COST_RET * nr + COST_APX - 1) / COST_APX);
 }
 
+#ifndef DQ4_W
+#define DQ4_W 12
+#define DQ4_E 3
+#endif
 template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
+    static constexpr int WARPS = EXACT || ROPE ? 8 : DQ4_W;
+    static constexpr int ENTRIES = EXACT || ROPE ? 4 : DQ4_E;          // of a warp's ring, a tile each
     static constexpr int THREADS = 32 * WARPS;
-    static constexpr int SLOT_BYTES = 2 * q4::Row<D>::TILE;
-    static constexpr int POS_AT = q4::Row<D>::TILE;                    // of a key-only tile's positions, within a slot
-    static constexpr int SMEM_BYTES = WARPS * SLOTS * SLOT_BYTES;      // and behind them the prefix sums
+    static constexpr int POS_AT = q4::Row<D>::TILE;                    // of a key-only tile's positions, within an entry
+    static constexpr int ENTRY_BYTES = q4::Row<D>::TILE + (ROPE ? 4 * q4::ROWS : 0);
+    static constexpr int SMEM_BYTES = WARPS * ENTRIES * ENTRY_BYTES;   // and behind them the prefix sums
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
 };
 
+// Not volatile, like the transposes: the compiler may move them past one another, so that one's operands are on their way during the next.
 __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile(
+    asm(
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ uint32_t transpose(uint32_t a) {
     uint32_t r;
-    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(a));
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;\n" : "=r"(r) : "r"(a));
     return r;
 }
 __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
@@ -149,8 +161,9 @@ struct Runs {
     }
 };
 
-// What a slot holds, for its consumer: unit, rows that are there, tier, whether it is the unit's first tile.
-struct Tile { int unit, rows, apx, first; };
+// What an entry of a ring holds, for its consumer: unit, rows that are there, whether it is the unit's first tile.
+enum Kind { KEYS, VALUES, KEY_ONLY };
+struct Entry { int unit, rows, kind, first; };
 
 // N neighbouring numbers at a multiple of 16 bytes.
 template <int N> __device__ __forceinline__ void load_run(const float* p, float* x) {
@@ -175,9 +188,10 @@ __global__ void __launch_bounds__(Cfg<T, D, ROPE, EXACT>::THREADS, 1)
 decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* ws, int* fault, RopePhases phases) {
     using C = Cfg<T, D, ROPE, EXACT>;
     using R = q4::Row<D>;
+    constexpr int WARPS = C::WARPS, ENTRIES = C::ENTRIES;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ __align__(8) uint64_t full[WARPS][SLOTS];
-    __shared__ Tile tiles[WARPS][SLOTS];
+    __shared__ __align__(8) uint64_t full[WARPS][ENTRIES];
+    __shared__ Entry entries[WARPS][ENTRIES];
     __shared__ int64_t sums[WARPS];
     __shared__ uint32_t phase32[ROPE ? D / 2 : 1];
     __shared__ RopePhase phase64[ROPE && EXACT ? D / 2 : 1];
@@ -185,7 +199,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
     if (lane == 0) {
 #pragma unroll
-        for (int s = 0; s < SLOTS; ++s) tma::mbar_init(&full[wid][s], 1);
+        for (int s = 0; s < ENTRIES; ++s) tma::mbar_init(&full[wid][s], 1);
         tma::mbar_fence_init();
     }
     if constexpr (ROPE) {
@@ -228,58 +242,53 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
 
     float* records = reinterpret_cast<float*>(ws + prefix_bytes(c.batch));
     const int rec = 2 * tier_floats(g, D), heads = even_heads(g), units = c.batch * c.LH;
-    unsigned char* ring = smem + wid * SLOTS * C::SLOT_BYTES;
+    unsigned char* ring = smem + wid * ENTRIES * C::ENTRY_BYTES;
     const uint64_t policy = tma::policy_evict_first();
 
-    // ---- the producing side, SLOTS tiles ahead: `run` is where it is, `k` tiles of it are on their way, and lane l has the page of tile l of 32
+    // ---- the producing side, ENTRIES ahead: `run` is where it is, `k` tiles of it are on their way, and lane l has the page of tile l of 32
     Runs run;
     run.find(c, prefix, deal.begin(worker), deal.begin(worker + 1));
-    int k = 0, page = -1;
-    size_t row_at = 0;
+    int k = 0, page = -1, values = 0;
     auto issue = [&](int s) {
-        if ((k & 31) == 0) {
-            row_at = run.apx ? (size_t)run.b * c.apx_width + run.p : (size_t)run.b * c.ret_width + run.p;
-            if (k + lane < run.count) page = (run.apx ? c.apx_table : c.ret_table)[row_at + k + lane];
-        }
+        if ((k & 31) == 0 && k + lane < run.count && !values)
+            page = run.apx ? c.apx_table[(size_t)run.b * c.apx_width + run.p + k + lane] : c.ret_table[(size_t)run.b * c.ret_width + run.p + k + lane];
         const int at = __shfl_sync(0xffffffffu, page, k & 31);
         if (lane == 0) {
             const bool there = at >= 0 && at < (run.apx ? c.n_apx_pages : c.n_ret_pages);
             const int p = run.p + k;
             const size_t tile = (size_t)at * c.LH + run.lh;
-            tiles[wid][s] = Tile{run.b * c.LH + run.lh, there ? min((run.apx ? run.n_apx : run.n_ret) - p * q4::ROWS, (int)q4::ROWS) : 0, run.apx,
-                                 p == 0 && (!run.apx || run.n_ret == 0)};
+            entries[wid][s] = Entry{run.b * c.LH + run.lh, there ? min((run.apx ? run.n_apx : run.n_ret) - p * q4::ROWS, (int)q4::ROWS) : 0,
+                                    run.apx ? KEY_ONLY : values ? VALUES : KEYS, p == 0 && (!run.apx || run.n_ret == 0)};
             uint64_t* bar = &full[wid][s];
-            unsigned char* to = ring + s * C::SLOT_BYTES;
+            unsigned char* to = ring + s * C::ENTRY_BYTES;
             if (!there) {
                 tma::mbar_arrive(bar);
-            } else if (run.apx) {
-                tma::mbar_expect_tx(bar, R::TILE + (ROPE ? 4 * q4::ROWS : 0));
-                tma::load_bulk_hint(to, c.apx + tile * R::TILE, R::TILE, bar, policy);
-                if (ROPE) tma::load_bulk_hint(to + C::POS_AT, c.apx_pos + tile * q4::ROWS, 4 * q4::ROWS, bar, policy);
             } else {
-                tma::mbar_expect_tx(bar, 2 * R::TILE);
-                tma::load_bulk_hint(to, c.ret + tile * 2 * R::TILE, 2 * R::TILE, bar, policy);
+                tma::mbar_expect_tx(bar, R::TILE + (ROPE && run.apx ? 4 * q4::ROWS : 0));
+                tma::load_bulk_hint(to, run.apx ? c.apx + tile * R::TILE : c.ret + (2 * tile + values) * R::TILE, R::TILE, bar, policy);
+                if (ROPE && run.apx) tma::load_bulk_hint(to + C::POS_AT, c.apx_pos + tile * q4::ROWS, 4 * q4::ROWS, bar, policy);
             }
         }
-        if (++k == run.count) {
+        if (!run.apx) values ^= 1;
+        if (!values && ++k == run.count) {
             run.next(c, prefix);
             k = 0;
         }
     };
-    int ahead = 0;
+    int ahead = 0;                             // entries on their way or not yet done with
 #pragma unroll
-    for (int s = 0; s < SLOTS; ++s)
+    for (int s = 0; s < ENTRIES; ++s)
         if (run.count > 0) { issue(s); ++ahead; }
     __syncwarp();
 
     // ---- the consuming side
     uint32_t qb[C::Q_PARTS][C::O_TILES][2];
-    float fac[2] = {0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, O[C::O_TILES][4], L[4];
+    float fac[2] = {0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, O[C::O_TILES][4], L[2];
     auto clear = [&] {
         m[0] = m[1] = -INFINITY;
 #pragma unroll
         for (int t = 0; t < C::O_TILES; ++t) O[t][0] = O[t][1] = O[t][2] = O[t][3] = 0.f;
-        L[0] = L[1] = L[2] = L[3] = 0.f;
+        L[0] = L[1] = 0.f;
     };
     clear();
     // The queries of a unit as B fragments: head gid, the channels of piece tig.  Scaled so that the largest lies in [2^7, 2^8).
@@ -313,31 +322,109 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             }
         }
     };
-    // Rows 16 i + gid and 16 i + gid + 8 of a tile's 32 rows at `row0`, as A fragments.
-    auto load_rows = [&](const unsigned char* tile, int row0, uint32_t (&x)[2][2][C::PAIRS]) {
+    // Rows row0 + gid and row0 + gid + 8 of a tile as A fragments.
+    auto load_rows = [&](const unsigned char* tile, int row0, uint32_t (&x)[2][C::PAIRS]) {
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int h = 0; h < 2; ++h) {
+            const int row = row0 + 8 * h + gid;
+            uint32_t w[4];
+            if constexpr (D == 128) {
+                const uint4 v = *reinterpret_cast<const uint4*>(tile + row * R::CODES + tig * 16);
+                w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+            } else {
+                const uint2 v = *reinterpret_cast<const uint2*>(tile + row * R::CODES + tig * 8);
+                w[0] = v.x; w[1] = v.y;
+            }
+            const uint32_t s = *reinterpret_cast<const uint16_t*>(tile + R::SCALES_AT + row * R::GROUPS + 2 * (D == 128 ? tig : tig >> 1));
+            const uint32_t s2[2] = {(s & 0xffu) * 0x00800080u, (s >> 8) * 0x00800080u};
+#pragma unroll
+            for (int j = 0; j < D / 32; ++j) {
+                uint32_t p[4];
+                q4::decode_word(w[j], p);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x[h][4 * j + i] = mul_h2(p[i], s2[j / (D / 64)]);
+            }
+        }
+    };
+    // Logits of 16 keys, in chains of two products (EXACT) or of half of them.
+    auto logits = [&](const uint32_t (&x)[2][C::PAIRS], float (&S)[4]) {
+        S[0] = S[1] = S[2] = S[3] = 0.f;
+        constexpr int CHAIN = EXACT ? 2 : C::O_TILES / 2;
+#pragma unroll
+        for (int p = C::Q_PARTS - 1; p >= 0; --p)
+#pragma unroll
+            for (int t0 = 0; t0 < C::O_TILES; t0 += CHAIN) {
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = t0; t < t0 + CHAIN; ++t) mma(sum, x[0][2 * t], x[1][2 * t], x[0][2 * t + 1], x[1][2 * t + 1], qb[p][t][0], qb[p][t][1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) S[e] += sum[e];
+            }
+    };
+    // Weights of N x 16 keys, of which `rows` are there, from their logits, against the reference m (fac > 0); as B fragments.
+    auto weigh = [&](auto& S, int rows, auto& ph, auto& pl) {
+        constexpr int N = sizeof(S) / sizeof(S[0]);
+        if (rows < 16 * N) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (16 * i + 8 * (e >> 1) + gid >= rows) S[i][e] = -INFINITY;
+        }
+        float top[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            top[h] = fmaxf(S[0][h], S[0][2 + h]);
+#pragma unroll
+            for (int i = 1; i < N; ++i) top[h] = fmaxf(top[h], fmaxf(S[i][h], S[i][2 + h]));
+            top[h] *= fac[h];
+        }
+        if (__any_sync(0xffffffffu, top[0] > m[0] + SLACK || top[1] > m[1] + SLACK)) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int row = row0 + 16 * i + 8 * h + gid;
-                uint32_t w[4];
-                if constexpr (D == 128) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(tile + row * R::CODES + tig * 16);
-                    w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-                } else {
-                    const uint2 v = *reinterpret_cast<const uint2*>(tile + row * R::CODES + tig * 8);
-                    w[0] = v.x; w[1] = v.y;
-                }
-                const uint32_t s = *reinterpret_cast<const uint16_t*>(tile + R::SCALES_AT + row * R::GROUPS + 2 * (D == 128 ? tig : tig >> 1));
-                const uint32_t s2[2] = {(s & 0xffu) * 0x00800080u, (s >> 8) * 0x00800080u};
 #pragma unroll
-                for (int j = 0; j < D / 32; ++j) {
-                    uint32_t p[4];
-                    q4::decode_word(w[j], p);
+                for (int o = 4; o < 32; o <<= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], o));
+                const float now = fmaxf(m[h], top[h]), f = m[h] == now ? 1.f : tc::ex2(m[h] - now);
+                m[h] = now;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) x[i][h][4 * j + k] = mul_h2(p[k], s2[j / (D / 64)]);
+                for (int t = 0; t < C::O_TILES; ++t) { O[t][h] *= f; O[t][2 + h] *= f; }
+                L[h] *= f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float a = tc::ex2(fmaf(S[i][2 * h], fac[0], -m[0])), b = tc::ex2(fmaf(S[i][2 * h + 1], fac[1], -m[1]));
+                const uint32_t hi = pack_h2(a, b);
+                ph[i][h] = transpose(hi);
+                if constexpr (EXACT) {
+                    const float2 f = unpack_h2(hi);
+                    pl[i][h] = transpose(pack_h2(a - f.x, b - f.y));
                 }
             }
+    };
+    // Sums of 16 rows x, times their weights; lo: second parts of the rows, where there are any.
+    auto add_rows = [&](const uint32_t (&x)[2][C::PAIRS], const uint32_t (&ph)[2], const uint32_t (&pl)[2], const auto& lo, auto with_lo) {
+#pragma unroll
+        for (int t = 0; t < C::O_TILES; ++t) {
+            const uint32_t a0 = transpose(x[0][2 * t]), a1 = transpose(x[0][2 * t + 1]), a2 = transpose(x[1][2 * t]), a3 = transpose(x[1][2 * t + 1]);
+            if constexpr (EXACT) {
+                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                mma(sum, a0, a1, a2, a3, pl[0], pl[1]);
+                if constexpr (with_lo.value) mma(sum, transpose(lo[0][2 * t]), transpose(lo[0][2 * t + 1]), transpose(lo[1][2 * t]), transpose(lo[1][2 * t + 1]), ph[0], ph[1]);
+                mma(sum, a0, a1, a2, a3, ph[0], ph[1]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) O[t][e] += sum[e];
+            } else {
+                mma(O[t], a0, a1, a2, a3, ph[0], ph[1]);
+            }
+        }
+        constexpr uint32_t ONE = 0x3c003c00u;
+        float sum[4] = {0.f, 0.f, 0.f, 0.f};
+        if constexpr (EXACT) mma(sum, ONE, ONE, ONE, ONE, pl[0], pl[1]);
+        mma(sum, ONE, ONE, ONE, ONE, ph[0], ph[1]);
+        L[0] += sum[0]; L[1] += sum[1];
     };
 
     int unit = -1, apx = 0, wrote = 0, slot_rec = 0;
@@ -359,170 +446,114 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         if (!(wrote & 2)) put_tier(1, true);
     };
 
-    for (int i = 0; ahead > 0; ++i) {
-        const int s = i % SLOTS;
-        if (!tma::mbar_wait_warp(&full[wid][s], (i / SLOTS) & 1, fault, 21)) {
-            for (int k = i; k < i + ahead; ++k) tma::mbar_wait_warp(&full[wid][k % SLOTS], (k / SLOTS) & 1, fault, 21);     // copies in flight
-            return;
+    int at = 0, phase = 0;                                              // the entry at hand, and its barrier's phase
+    auto wait = [&] {
+        if (tma::mbar_wait_warp(&full[wid][at], phase, fault, 21)) return true;
+        for (; ahead > 0; --ahead) {                                   // copies in flight still land in this block's memory
+            tma::mbar_wait_warp(&full[wid][at], phase, fault, 21);
+            if (++at == ENTRIES) { at = 0; phase ^= 1; }
         }
-        const Tile tile = tiles[wid][s];
-        if (tile.unit != unit) {
+        return false;
+    };
+    auto release = [&] {
+        __syncwarp();                                                  // every lane has read the entry
+        --ahead;
+        if (run.count > 0) { issue(at); ++ahead; __syncwarp(); }
+        if (++at == ENTRIES) { at = 0; phase ^= 1; }
+    };
+    // What lies behind the last row may be no number: scales of zero there.
+    auto blank = [&](unsigned char* tile, int rows) {
+        for (int i = rows * R::GROUPS + lane; i < q4::ROWS * R::GROUPS; i += 32) tile[R::SCALES_AT + i] = 0;
+        asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
+        __syncwarp();
+    };
+    while (ahead > 0) {
+        if (!wait()) return;
+        const Entry entry = entries[wid][at];
+        const int tier = entry.kind == KEY_ONLY;
+        if (entry.unit != unit) {
             leave_unit();
-            unit = tile.unit; apx = tile.apx; wrote = 0;
-            slot_rec = tile.first ? unit : units + worker;
+            unit = entry.unit; apx = tier; wrote = 0;
+            slot_rec = entry.first ? unit : units + worker;
             clear();
             load_queries(unit);
-        } else if (tile.apx != apx) {
+        } else if (tier != apx) {
             put_tier(apx, false);
             wrote |= 1 << apx;
-            apx = tile.apx;
+            apx = tier;
             clear();
         }
-        unsigned char* at = ring + s * C::SLOT_BYTES;
-        if (tile.rows < q4::ROWS) {            // what lies behind the last row may be no number: scales of zero
-            for (int i = tile.rows * R::GROUPS + lane; i < q4::ROWS * R::GROUPS; i += 32) {
-                at[R::SCALES_AT + i] = 0;
-                if (!tile.apx) at[R::TILE + R::SCALES_AT + i] = 0;
+        unsigned char* tile = ring + at * C::ENTRY_BYTES;
+        if (!tier) {
+            uint32_t ph[4][2], pl[4][2];
+            if (entry.rows > 0) {
+                float S[4][4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t x[2][C::PAIRS];
+                    load_rows(tile, 16 * i, x);
+                    logits(x, S[i]);
+                }
+                weigh(S, entry.rows, ph, pl);
             }
-            asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
-            __syncwarp();
-        }
+            release();
+            if (!wait()) return;
+            tile = ring + at * C::ENTRY_BYTES;
+            if (entry.rows > 0) {
+                if (entry.rows < q4::ROWS) blank(tile, entry.rows);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    uint32_t x[2][C::PAIRS];
+                    load_rows(tile, 16 * i, x);
+                    add_rows(x, ph[i], pl[i], x, std::false_type());
+                }
+            }
+        } else {
+            if (entry.rows < q4::ROWS) blank(tile, entry.rows);
 #pragma unroll 1
-        for (int row0 = 0; row0 < tile.rows; row0 += 32) {
-            const int rows = tile.rows - row0;
-            uint32_t x[2][2][C::PAIRS];
-            load_rows(at, row0, x);
-            // ---- logits, in chains of two products (EXACT) or of half of them
-            float S[2][4];
+            for (int row0 = 0; row0 < entry.rows; row0 += 16) {
+                uint32_t x[2][C::PAIRS], ph[1][2], pl[1][2], lo[ROPE && EXACT ? 2 : 1][ROPE && EXACT ? C::PAIRS : 1];
+                float S[1][4];
+                load_rows(tile, row0, x);
+                logits(x, S[0]);
+                weigh(S, entry.rows - row0, ph, pl);
+                if constexpr (ROPE) {
 #pragma unroll
-            for (int i = 0; i < 2; ++i) S[i][0] = S[i][1] = S[i][2] = S[i][3] = 0.f;
-            constexpr int CHAIN = EXACT ? 2 : C::O_TILES / 2;
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t pos = (uint32_t)reinterpret_cast<const int32_t*>(tile + C::POS_AT)[row0 + 8 * h + gid];
 #pragma unroll
-            for (int p = C::Q_PARTS - 1; p >= 0; --p)
-#pragma unroll
-                for (int t0 = 0; t0 < C::O_TILES; t0 += CHAIN)
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                        for (int t = t0; t < t0 + CHAIN; ++t)
-                            mma(sum, x[i][0][2 * t], x[i][1][2 * t], x[i][0][2 * t + 1], x[i][1][2 * t + 1], qb[p][t][0], qb[p][t][1]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) S[i][e] += sum[e];
-                    }
-            if (rows < 32) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (16 * i + 8 * (e >> 1) + gid >= rows) S[i][e] = -INFINITY;
-            }
-            // ---- softmax against the reference m (fac > 0)
-            float top[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) top[h] = fmaxf(fmaxf(S[0][h], S[0][2 + h]), fmaxf(S[1][h], S[1][2 + h])) * fac[h];
-            if (__any_sync(0xffffffffu, top[0] > m[0] + SLACK || top[1] > m[1] + SLACK)) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                    for (int o = 4; o < 32; o <<= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], o));
-                    const float now = fmaxf(m[h], top[h]), f = m[h] == now ? 1.f : tc::ex2(m[h] - now);
-                    m[h] = now;
-#pragma unroll
-                    for (int t = 0; t < C::O_TILES; ++t) { O[t][h] *= f; O[t][2 + h] *= f; }
-                    L[h] *= f; L[2 + h] *= f;
-                }
-            }
-            uint32_t ph[2][2], pl[2][2];
-#pragma unroll
-            for (int k = 0; k < 2; ++k)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const float a = tc::ex2(fmaf(S[k][2 * h], fac[0], -m[0])), b = tc::ex2(fmaf(S[k][2 * h + 1], fac[1], -m[1]));
-                    const uint32_t hi = pack_h2(a, b);
-                    ph[k][h] = transpose(hi);
-                    if constexpr (EXACT) {
-                        const float2 f = unpack_h2(hi);
-                        pl[k][h] = transpose(pack_h2(a - f.x, b - f.y));
-                    }
-                }
-            if (!tile.apx) load_rows(at + R::TILE, row0, x);
-            uint32_t lo[2][2][ROPE && EXACT ? C::PAIRS : 1];           // second parts of keys turned back
-            if constexpr (ROPE) {
-                if (tile.apx) {
-#pragma unroll
-                    for (int k = 0; k < 2; ++k)
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            const int r = 16 * k + 8 * h + gid;
-                            const uint32_t pos = r < rows ? (uint32_t)reinterpret_cast<const int32_t*>(at + C::POS_AT)[row0 + r] : 0u;
-#pragma unroll
-                            for (int j = 0; j < C::PAIRS / 2; ++j) {
-                                const int ch = tig * (D / 8) + 2 * j;
-                                uint32_t &u = x[k][h][j], &v = x[k][h][C::PAIRS / 2 + j];
-                                if constexpr (EXACT) {
-                                    uint64_t cs, sn;
-                                    rope_cos_sin2(rope_angle((int32_t)pos, phase64[ch]), rope_angle((int32_t)pos, phase64[ch + 1]), cs, sn);
-                                    const float2 uf = unpack_h2(u), vf = unpack_h2(v);
-                                    const uint64_t u2 = tc::pack2(uf.x, uf.y), v2 = tc::pack2(vf.x, vf.y);
-                                    auto parts = [](uint64_t z, uint32_t& hi, uint32_t& low) {
-                                        float a, b;
-                                        tc::unpack2(z, a, b);
-                                        hi = pack_h2(a, b);
-                                        const float2 f = unpack_h2(hi);
-                                        low = pack_h2(a - f.x, b - f.y);
-                                    };
-                                    const uint64_t neg = tc::pack2(-1.f, -1.f);
-                                    parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[k][h][j]);
-                                    parts(tc::fma2(u2, tc::mul2(sn, neg), tc::mul2(v2, cs)), v, lo[k][h][C::PAIRS / 2 + j]);
-                                } else {
-                                    float c0, s0, c1, s1;
-                                    rope_phase32_cos_sin(pos, phase32[ch], c0, s0);
-                                    rope_phase32_cos_sin(pos, phase32[ch + 1], c1, s1);
-                                    const uint32_t cs = pack_h2(c0, c1), sn = pack_h2(s0, s1), a = u, b = v;
-                                    u = fma_h2(a, cs, mul_h2(b, sn));
-                                    v = fma_h2(b, cs, mul_h2(a ^ 0x80008000u, sn));
-                                }
+                        for (int j = 0; j < C::PAIRS / 2; ++j) {
+                            const int ch = tig * (D / 8) + 2 * j;
+                            uint32_t &u = x[h][j], &v = x[h][C::PAIRS / 2 + j];
+                            if constexpr (EXACT) {
+                                uint64_t cs, sn;
+                                rope_cos_sin2(rope_angle((int32_t)pos, phase64[ch]), rope_angle((int32_t)pos, phase64[ch + 1]), cs, sn);
+                                const float2 uf = unpack_h2(u), vf = unpack_h2(v);
+                                const uint64_t u2 = tc::pack2(uf.x, uf.y), v2 = tc::pack2(vf.x, vf.y);
+                                auto parts = [](uint64_t z, uint32_t& hi, uint32_t& low) {
+                                    float a, b;
+                                    tc::unpack2(z, a, b);
+                                    hi = pack_h2(a, b);
+                                    const float2 f = unpack_h2(hi);
+                                    low = pack_h2(a - f.x, b - f.y);
+                                };
+                                parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
+                                parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);
+                            } else {
+                                float c0, s0, c1, s1;
+                                rope_phase32_cos_sin(pos, phase32[ch], c0, s0);
+                                rope_phase32_cos_sin(pos, phase32[ch + 1], c1, s1);
+                                const uint32_t cs = pack_h2(c0, c1), sn = pack_h2(s0, s1), a = u, b = v;
+                                u = fma_h2(a, cs, mul_h2(b, sn));
+                                v = fma_h2(b, cs, mul_h2(a ^ 0x80008000u, sn));
                             }
                         }
-                }
-            }
-            const bool two = ROPE && EXACT && tile.apx;
-#pragma unroll
-            for (int t = 0; t < C::O_TILES; ++t) {
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const uint32_t a0 = transpose(x[k][0][2 * t]), a1 = transpose(x[k][0][2 * t + 1]), a2 = transpose(x[k][1][2 * t]),
-                                   a3 = transpose(x[k][1][2 * t + 1]);
-                    if constexpr (EXACT) {
-                        mma(sum, a0, a1, a2, a3, pl[k][0], pl[k][1]);
-                        if constexpr (ROPE)
-                            if (two)
-                                mma(sum, transpose(lo[k][0][2 * t]), transpose(lo[k][0][2 * t + 1]), transpose(lo[k][1][2 * t]), transpose(lo[k][1][2 * t + 1]),
-                                    ph[k][0], ph[k][1]);
-                        mma(sum, a0, a1, a2, a3, ph[k][0], ph[k][1]);
-                    } else {
-                        mma(O[t], a0, a1, a2, a3, ph[k][0], ph[k][1]);
                     }
                 }
-                if constexpr (EXACT) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) O[t][e] += sum[e];
-                }
+                add_rows(x, ph[0], pl[0], lo, std::bool_constant<ROPE && EXACT>());
             }
-            constexpr uint32_t ONE = 0x3c003c00u;
-            float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                if constexpr (EXACT) mma(sum, ONE, ONE, ONE, ONE, pl[k][0], pl[k][1]);
-                mma(sum, ONE, ONE, ONE, ONE, ph[k][0], ph[k][1]);
-            }
-            L[0] += sum[0]; L[1] += sum[1];
         }
-        __syncwarp();                                                  // every lane has read the slot
-        --ahead;
-        if (run.count > 0) { issue(s); ++ahead; __syncwarp(); }
+        release();
     }
     leave_unit();
 }
