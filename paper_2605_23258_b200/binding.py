@@ -258,7 +258,7 @@ def _marshal():
             loader = importlib.machinery.ExtensionFileLoader(f"{__package__}._marshal", path)
             module = importlib.util.module_from_spec(importlib.util.spec_from_file_location(loader.name, path, loader=loader))
             loader.exec_module(module)
-            module.bind(lib._handle, Shape, Budget, Cache)
+            module.bind(lib._handle, Shape, Budget, Cache, Q4Cache)
         except ImportError as e:
             warnings.warn(f"the extension module {path} cannot be used ({e}): every call goes through ctypes, at some microseconds more; "
                           "build it with `python -m paper_2605_23258_b200.build`", RuntimeWarning, stacklevel=3)
@@ -638,6 +638,11 @@ def alloc_q4_cache(shape: Shape, ret_pages: int, apx_pages: int, ret_width: int,
 
 def vector_block_tables(lengths, added, page_rows: int, table, free_pages, n_free, new_lengths, new_n_free, first_row, row_start, slots=None, stream=None):
     """Tables, lengths and slots after request b changed by added[b] rows; new_lengths may be lengths and new_n_free n_free."""
+    rc = (_marshal_module or _marshal()).block_tables(lengths, added, page_rows, table, free_pages, n_free, new_lengths, new_n_free, first_row, row_start, slots, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_block_tables")
+        return
     if table.dim() != 2:
         raise ValueError("table must be [batch][width]")
     B, i32 = table.shape[0], torch.int32
@@ -651,6 +656,11 @@ def vector_block_tables(lengths, added, page_rows: int, table, free_pages, n_fre
 
 
 def vector_compact_q4(shape: Shape, budget: Budget, K, V, ret_idx, apx_idx, cache: Q4Cache, ret_slots, apx_slots, stream=None):
+    rc = (_marshal_module or _marshal()).compact_q4(shape, budget, K, V, ret_idx, apx_idx, cache, ret_slots, apx_slots, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_compact_q4")
+        return
     U, B, d = shape.units, shape.batch, shape.head_dim
     rc = load_library().vector_compact_q4(shape._p(), budget._p(), _sized(K, shape.torch_dtype, U * budget.n_tokens * d, "K"),
                                           _sized(V, shape.torch_dtype, U * budget.n_tokens * d, "V"),
@@ -662,6 +672,11 @@ def vector_compact_q4(shape: Shape, budget: Budget, K, V, ret_idx, apx_idx, cach
 
 def vector_append_q4(shape: Shape, cache: Q4Cache, k_new, v_new, row_start, slots, pos=None, stream=None):
     """k_new, v_new [U][d]: the rows of sequence b go to slots[row_start[b]], or to slots[b] where row_start is None."""
+    rc = (_marshal_module or _marshal()).append_q4(shape, cache, k_new, v_new, row_start, slots, pos, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_append_q4")
+        return
     B, n = shape.batch, shape.units * shape.head_dim
     rc = load_library().vector_append_q4(shape._p(), _q4(shape, cache), _sized(k_new, shape.torch_dtype, n, "k_new"), _sized(v_new, shape.torch_dtype, n, "v_new"),
                                          None if row_start is None else _sized(row_start, torch.int32, B + 1, "row_start"),
@@ -671,6 +686,11 @@ def vector_append_q4(shape: Shape, cache: Q4Cache, k_new, v_new, row_start, slot
 
 def vector_read_q4(shape: Shape, cache: Q4Cache, ret_slots=None, ret_k=None, ret_v=None, apx_slots=None, apx_k=None, stream=None):
     """Rows of slots [batch][n] as values [U][n][d]: retained ones to ret_k and ret_v, key-only ones to apx_k."""
+    rc = (_marshal_module or _marshal()).read_q4(shape, cache, ret_slots, ret_k, ret_v, apx_slots, apx_k, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_read_q4")
+        return
     U, B, d, dt = shape.units, shape.batch, shape.head_dim, shape.torch_dtype
     n_ret, n_apx = (0 if t is None else t.numel() // B for t in (ret_slots, apx_slots))
     rc = load_library().vector_read_q4(shape._p(), _q4(shape, cache), _sized(ret_slots, torch.int32, B * n_ret, "ret_slots"), n_ret,
@@ -684,6 +704,11 @@ def vector_decode_q4_workspace_bytes(shape: Shape) -> int:
 
 
 def vector_decode_attn_q4(shape: Shape, q, cache: Q4Cache, W, out, ws=None, stream=None):
+    rc = (_marshal_module or _marshal()).decode_attn_q4(shape, q, cache, W, out, ws, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_decode_attn_q4")
+        return
     wp, wn = _ws(ws)
     if out.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("out must be fp32 or bf16")

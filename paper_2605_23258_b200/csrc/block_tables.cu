@@ -56,21 +56,6 @@ __device__ __forceinline__ int64_t scan(int64_t x, int64_t* warps, int64_t& tota
     return s - x + (wid ? before : 0);
 }
 
-// f(i, row, at) for i in [0, n) of every lane's own n, row and at: a lane alone while they are few, all lanes together for the long ones.
-template <typename F>
-__device__ __forceinline__ void each(int n, int32_t* row, int64_t at, F f) {
-    constexpr int FEW = 4;
-    if (n <= FEW)
-        for (int i = 0; i < n; ++i) f(i, row, at);
-    for (unsigned big = __ballot_sync(0xffffffffu, n > FEW); big; big &= big - 1) {
-        const int src = __ffs(big) - 1;
-        const int m = __shfl_sync(0xffffffffu, n, src);
-        int32_t* r = (int32_t*)__shfl_sync(0xffffffffu, (unsigned long long)row, src);
-        const int64_t p = __shfl_sync(0xffffffffu, at, src);
-        for (int i = threadIdx.x & 31; i < m; i += 32) f(i, r, p);
-    }
-}
-
 // The request that row k of the added rows belongs to: the last b in [lo, hi) with start[b] <= k.
 __device__ __forceinline__ int request_of(const int32_t* start, int lo, int hi, int64_t k) {
     while (hi - lo > 1) {
@@ -80,14 +65,37 @@ __device__ __forceinline__ int request_of(const int32_t* start, int lo, int hi, 
     }
     return lo;
 }
-// Slot of the k-th added row, which is one of request b's.
-__device__ __forceinline__ int32_t slot_of(const Args& a, int b, int64_t start, int64_t k) {
-    const int64_t row = a.first_row[b] + (k - start);
-    if (row >= a.new_lengths[b]) return -1;                      // no page was left for it
-    const uint32_t page = (uint32_t)row / (uint32_t)a.page_rows;
-    const int64_t at = a.table[(size_t)b * a.width + page];
-    const int64_t slot = at * a.page_rows + (int64_t)((uint32_t)row - page * (uint32_t)a.page_rows);
-    return at < 0 || slot > 0x7fffffffLL ? -1 : (int32_t)slot;
+// Slot of row `row` in page `page`, -1 where that is none.
+__device__ __forceinline__ int32_t slot_of(int64_t page, int64_t row, int32_t page_rows) {
+    const int64_t slot = page * page_rows + (int64_t)((uint32_t)row % (uint32_t)page_rows);
+    return page < 0 || slot > 0x7fffffffLL ? -1 : (int32_t)slot;
+}
+__device__ __forceinline__ int32_t slot_of_row(const Args& a, int b, int64_t row, int64_t rows) {
+    if (row >= rows) return -1;                                  // no page was left for it
+    return slot_of(a.table[(size_t)b * a.width + (uint32_t)row / (uint32_t)a.page_rows], row, a.page_rows);
+}
+
+// Moves pages between the tables' rows and the stack, one page a thread and step, MOVES steps' loads in flight: page e of `total`, which is the
+// i-th of request b0 + k (starts[k] <= e, i = e - starts[k]), lies at entry first[k] + i of the request's row.  f(entry, e).
+template <typename Load, typename Store>
+__device__ __forceinline__ void move_pages(const Args& a, int b0, int n, int total, const int32_t* starts, const int32_t* first, Load load, Store store) {
+    constexpr int MOVES = 4;
+    for (int e0 = threadIdx.x; e0 < total; e0 += MOVES * THREADS) {
+        int32_t v[MOVES];
+        int32_t* entry[MOVES];
+#pragma unroll
+        for (int j = 0; j < MOVES; ++j) {
+            const int e = e0 + j * THREADS;
+            if (e < total) {
+                const int k = request_of(starts, 0, n, e);
+                entry[j] = a.table + (size_t)(b0 + k) * a.width + first[k] + (e - starts[k]);
+                v[j] = load(entry[j], e);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < MOVES; ++j)
+            if (e0 + j * THREADS < total) store(entry[j], e0 + j * THREADS, v[j]);
+    }
 }
 
 __global__ void __launch_bounds__(THREADS)
@@ -95,29 +103,30 @@ block_tables_plan(Args a, int with_slots) {
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     __shared__ int64_t warps[32];
-    __shared__ int32_t starts[THREADS + 1];
+    __shared__ int32_t starts[THREADS], first[THREADS], olds[THREADS], news[THREADS];
     const int t = threadIdx.x;
     int64_t height = min(max((int64_t)a.n_free[0], (int64_t)0), (int64_t)a.cap_free);
 
     // ---- released pages go on the stack, a request's in the order of its table
     int64_t total = 0;
     for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
-        const int b = b0 + t;
+        const int b = b0 + t, n = min(a.batch - b0, THREADS);
         Change c = {};
         if (b < a.batch) c = change_of(a, b);
         const int back = max(c.have - c.want, 0);
         if (!__syncthreads_or(back > 0)) continue;
-        const int64_t at = height + scan(back, warps, total);
-        each(back, a.table + (size_t)b * a.width + c.want, at, [&](int i, int32_t* row, int64_t p) {
-            if (p + i < a.cap_free) a.stack[p + i] = row[i];
-        });
+        starts[t] = (int32_t)scan(back, warps, total);
+        first[t] = c.want;
+        __syncthreads();
+        move_pages(a, b0, n, (int)min(total, (int64_t)a.cap_free - height), starts, first, [&](const int32_t* entry, int) { return *entry; },
+                   [&](int32_t*, int e, int32_t v) { a.stack[height + e] = v; });
         height = min(height + total, (int64_t)a.cap_free);
+        __syncthreads();
     }
-    __syncthreads();
     // ---- wanted pages come off it, as far as they go; lengths and the rows' starts
     int64_t needed = 0, added = 0;
     for (int b0 = 0; b0 < a.batch; b0 += THREADS) {
-        const int b = b0 + t;
+        const int b = b0 + t, n = min(a.batch - b0, THREADS);
         Change c = {};
         int grow = 0;
         if (b < a.batch) { c = change_of(a, b); grow = a.added[b]; }
@@ -126,30 +135,37 @@ block_tables_plan(Args a, int with_slots) {
         added += total;
         int64_t before = needed;
         if (__syncthreads_or(need > 0)) {
-            before += scan(need, warps, total);
+            const int64_t mine = scan(need, warps, total);
+            before += mine;
+            starts[t] = (int32_t)mine;
+            first[t] = c.have;
+            __syncthreads();
+            const int64_t top = height - 1 - needed;
+            move_pages(a, b0, n, (int)max(min(total, top + 1), (int64_t)0), starts, first, [&](const int32_t*, int e) { return a.stack[top - e]; },
+                       [&](int32_t* entry, int, int32_t v) { *entry = v; });
             needed += total;
+            __syncthreads();
         }
-        const int got = (int)min((int64_t)need, max(height - before, (int64_t)0));
-        each(got, a.table + (size_t)b * a.width + c.have, height - 1 - before, [&](int i, int32_t* row, int64_t p) { row[i] = a.stack[p - i]; });
         if (b < a.batch) {
-            const int32_t s = (int32_t)min(start, (int64_t)0x7fffffff);
+            const int got = (int)min((int64_t)need, max(height - before, (int64_t)0));
+            const int32_t s = (int32_t)min(start, (int64_t)0x7fffffff), rows = (int32_t)(grow > 0 ? min(c.rows, (int64_t)(c.have + got) * a.page_rows) : c.rows);
             a.first_row[b] = (int32_t)c.old_rows;
             a.row_start[b] = s;
-            a.new_lengths[b] = (int32_t)(grow > 0 ? min(c.rows, (int64_t)(c.have + got) * a.page_rows) : c.rows);
-            if (with_slots) starts[t] = s;
+            a.new_lengths[b] = rows;
+            if (with_slots) { starts[t] = s; olds[t] = (int32_t)c.old_rows; news[t] = rows; }
         }
     }
     if (t == 0) {
         a.row_start[a.batch] = (int32_t)min(added, (int64_t)0x7fffffff);
         a.new_n_free[0] = (int32_t)(height - min(needed, height));
     }
-    if (!with_slots) return;
+    if (!with_slots) return;                                     // with them the requests are one round's
     __syncthreads();
     for (int64_t k = t; k < a.n_slots; k += THREADS) {
         int32_t slot = -1;
         if (k < added) {
             const int b = request_of(starts, 0, a.batch, k);
-            slot = slot_of(a, b, starts[b], k);
+            slot = slot_of_row(a, b, olds[b] + (k - starts[b]), news[b]);
         }
         a.slots[k] = slot;
     }
@@ -181,7 +197,7 @@ block_tables_slots(Args a) {
         for (int i = 0; i < 4; ++i) {
             if (k + i >= added) break;
             if (a.row_start[b + 1] <= k + i) b = request_of(a.row_start, b + 1, a.batch, k + i);
-            got[i] = slot_of(a, b, a.row_start[b], k + i);
+            got[i] = slot_of_row(a, b, a.first_row[b] + (k + i - a.row_start[b]), a.new_lengths[b]);
         }
     }
     if (k + 4 <= a.n_slots && ((uintptr_t)a.slots & 15) == 0) {

@@ -72,6 +72,8 @@ __device__ __forceinline__ int tile_from(int64_t r, int nr) {
 
 #ifndef DQ4_W
 #define DQ4_W 12
+#endif
+#ifndef DQ4_E
 #define DQ4_E 3
 #endif
 template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
@@ -455,11 +457,10 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         }
         return false;
     };
-    auto release = [&] {
+    auto release = [&](int s) {
         __syncwarp();                                                  // every lane has read the entry
         --ahead;
-        if (run.count > 0) { issue(at); ++ahead; __syncwarp(); }
-        if (++at == ENTRIES) { at = 0; phase ^= 1; }
+        if (run.count > 0) { issue(s); ++ahead; __syncwarp(); }
     };
     // What lies behind the last row may be no number: scales of zero there.
     auto blank = [&](unsigned char* tile, int rows) {
@@ -485,29 +486,29 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         }
         unsigned char* tile = ring + at * C::ENTRY_BYTES;
         if (!tier) {
-            uint32_t ph[4][2], pl[4][2];
-            if (entry.rows > 0) {
-                float S[4][4];
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t x[2][C::PAIRS];
-                    load_rows(tile, 16 * i, x);
-                    logits(x, S[i]);
-                }
-                weigh(S, entry.rows, ph, pl);
-            }
-            release();
+            const unsigned char* keys = tile;
+            const int of_keys = at;
+            if (++at == ENTRIES) { at = 0; phase ^= 1; }
             if (!wait()) return;
             tile = ring + at * C::ENTRY_BYTES;
-            if (entry.rows > 0) {
-                if (entry.rows < q4::ROWS) blank(tile, entry.rows);
+            if (entry.rows < q4::ROWS) blank(tile, entry.rows);
+#pragma unroll 1
+            for (int row0 = 0; row0 < entry.rows; row0 += 32) {
+                uint32_t x[2][C::PAIRS], ph[2][2], pl[2][2];
+                float S[2][4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    uint32_t x[2][C::PAIRS];
-                    load_rows(tile, 16 * i, x);
+                for (int i = 0; i < 2; ++i) {
+                    load_rows(keys, row0 + 16 * i, x);
+                    logits(x, S[i]);
+                }
+                weigh(S, entry.rows - row0, ph, pl);
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    load_rows(tile, row0 + 16 * i, x);
                     add_rows(x, ph[i], pl[i], x, std::false_type());
                 }
             }
+            release(of_keys);
         } else {
             if (entry.rows < q4::ROWS) blank(tile, entry.rows);
 #pragma unroll 1
@@ -553,7 +554,8 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 add_rows(x, ph[0], pl[0], lo, std::bool_constant<ROPE && EXACT>());
             }
         }
-        release();
+        release(at);
+        if (++at == ENTRIES) { at = 0; phase ^= 1; }
     }
     leave_unit();
 }

@@ -20,7 +20,8 @@ namespace {
 
 #define ENTRY_POINTS(X) \
     X(vector_score) X(vector_route) X(vector_route_layer) X(vector_compact) X(vector_compact_layer) X(vector_append) X(vector_decode_attn) \
-        X(vector_decode_attn_layer) X(vector_decode_attn_static)
+        X(vector_decode_attn_layer) X(vector_decode_attn_static) X(vector_block_tables) X(vector_compact_q4) X(vector_append_q4) X(vector_read_q4) \
+        X(vector_decode_attn_q4) X(vector_q4_tile_bytes)
 #define POINTER(name) decltype(&::name) p_##name = nullptr;
 ENTRY_POINTS(POINTER)
 
@@ -51,12 +52,14 @@ struct Class {
         return true;
     }
 };
-Class shape_class, budget_class, cache_class;
+Class shape_class, budget_class, cache_class, q4_cache_class;
 enum Name { BATCH, N_LAYERS, N_Q_HEADS, N_KV_HEADS, HEAD_DIM, DTYPE, WINDOW, POOL_KERNEL, SM_SCALE, ROPE_ENABLED, ROPE_THETA, N_TOKENS,
-            N_BUDGET_PAIRS, N_A, N_POOL, N_APX, N_RET, N_EVICT, RET_K, RET_V, APX_K, RET_POS, APX_POS, NAMES };
+            N_BUDGET_PAIRS, N_A, N_POOL, N_APX, N_RET, N_EVICT, RET_K, RET_V, APX_K, RET_POS, APX_POS,
+            RET_PAGES, APX_PAGES, RET_TABLE, APX_TABLE, RET_LEN, APX_LEN, NAMES };
 const char* const spelled[NAMES] = {"batch", "n_layers", "n_q_heads", "n_kv_heads", "head_dim", "dtype", "window", "pool_kernel", "sm_scale",
                                     "rope_enabled", "rope_theta", "n_tokens", "n_budget_pairs", "n_a", "n_pool", "n_apx", "n_ret",
-                                    "n_evict", "ret_k", "ret_v", "apx_k", "ret_pos", "apx_pos"};
+                                    "n_evict", "ret_k", "ret_v", "apx_k", "ret_pos", "apx_pos", "ret_pages", "apx_pages", "ret_table", "apx_table", "ret_len",
+                                    "apx_len"};
 PyObject* name[NAMES];
 
 struct Ref {                                            // an owned reference, or none
@@ -115,6 +118,18 @@ struct Reader {
         return t && need(t->is_cuda() && t->is_contiguous() && t->scalar_type() == type) ? t->data_ptr() : nullptr;
     }
     void* optional(PyObject* o, at::ScalarType type) { return o == Py_None ? nullptr : device(o, type); }
+    // A tensor of n elements at least; null where there are none to have.
+    void* sized(PyObject* o, at::ScalarType type, int64_t n) {
+        if (n == 0) return nullptr;
+        void* p = device(o, type);
+        return plain && need(tensor(o)->numel() >= n) ? p : nullptr;
+    }
+    int32_t* ints(PyObject* o, int64_t n) { return (int32_t*)sized(o, at::kInt, n); }
+    int32_t* optional_ints(PyObject* o, int64_t n) { return o == Py_None ? nullptr : ints(o, n); }
+    int64_t numel(PyObject* o) {
+        const at::Tensor* t = o == Py_None ? nullptr : tensor(o);
+        return t ? t->numel() : 0;
+    }
     Workspace workspace(PyObject* o) {
         Workspace w;
         w.p = optional(o, at::kByte);
@@ -182,7 +197,44 @@ struct Reader {
         c.n_apx = field(o, N_APX);
         return c;
     }
+    // attends: with the tables and lengths, which attention alone reads.
+    vector_q4_cache q4_cache(PyObject* o, const vector_shape& s, bool attends) {
+        vector_q4_cache c = {};
+        if (!plain || !need(q4_cache_class.covers(o))) return c;
+        const int64_t LH = (int64_t)s.n_layers * s.n_kv_heads, tile = (int64_t)p_vector_q4_tile_bytes(&s);
+        auto pages = [&](Name n, int64_t bytes, int64_t* count) -> void* {
+            const Ref r(attr(o, n));
+            void* p = plain ? device(r.o, at::kByte) : nullptr;
+            if (!plain) return nullptr;
+            const at::Tensor* t = tensor(r.o);
+            if (!need(t->dim() == 3 && t->size(1) == LH && t->size(2) == bytes)) return nullptr;
+            *count = t->size(0);
+            return p;
+        };
+        c.ret_pages = pages(RET_PAGES, 2 * tile, &c.n_ret_pages);
+        c.apx_pages = pages(APX_PAGES, tile, &c.n_apx_pages);
+        auto positions = [&](Name n, int64_t count) -> int32_t* {
+            const Ref r(attr(o, n));
+            return plain ? optional_ints(r.o, count * LH * VECTOR_PAGE_ROWS) : nullptr;
+        };
+        c.ret_pos = positions(RET_POS, c.n_ret_pages);
+        c.apx_pos = positions(APX_POS, c.n_apx_pages);
+        auto tables = [&](Name n, Name len, const int32_t** table, const int32_t** lens, int32_t* width) {
+            const Ref r(attr(o, n)), l(attr(o, len));
+            if (!plain) return;
+            *table = (int32_t*)device(r.o, at::kInt);
+            if (!plain || !need(tensor(r.o)->dim() == 2 && tensor(r.o)->size(0) >= s.batch && tensor(r.o)->size(1) <= 0x7fffffffLL)) return;
+            *width = (int32_t)tensor(r.o)->size(1);
+            *lens = ints(l.o, s.batch);
+        };
+        if (attends) {
+            tables(RET_TABLE, RET_LEN, &c.ret_table, &c.ret_len, &c.ret_width);
+            tables(APX_TABLE, APX_LEN, &c.apx_table, &c.apx_len, &c.apx_width);
+        }
+        return c;
+    }
 };
+int64_t units_of(const vector_shape& s) { return (int64_t)s.batch * s.n_layers * s.n_kv_heads; }
 
 // What `call` returns as a Python integer; None where the plain case does not hold.
 template <typename F>
@@ -323,10 +375,81 @@ METHOD(append_rows) {                                   // shape, cache, k_new, 
         return rc;
     });
 }
-// The library's entry points, by the handle of the library that ctypes has loaded, and the classes of the three structs.
+METHOD(block_tables) {                                  // lengths, added, page_rows, table, free, n_free, new_lengths, new_n_free, first_row, row_start, slots, stream
+    return plain(n, 12, [&](Reader& r) {
+        const int32_t* table = (const int32_t*)r.device(a[3], at::kInt);
+        const at::Tensor* t = r.tensor(a[3]);
+        if (!r.plain || !r.need(t->dim() == 2 && t->size(0) <= 0x7fffffffLL && t->size(1) <= 0x7fffffffLL)) return 0L;
+        const int64_t B = t->size(0), width = t->size(1), n_slots = r.numel(a[10]);
+        const int32_t *lengths = r.ints(a[0], B), *added = r.ints(a[1], B), *n_free = r.ints(a[5], 1);
+        const int32_t page_rows = r.integer32(a[2]);
+        int32_t* stack = (int32_t*)r.device(a[4], at::kInt);
+        const int64_t cap = r.plain ? r.tensor(a[4])->numel() : 0;
+        r.need(cap <= 0x7fffffffLL);
+        int32_t *new_lengths = r.ints(a[6], B), *new_n_free = r.ints(a[7], 1), *first = r.ints(a[8], B), *start = r.ints(a[9], B + 1), *slots = r.ints(a[10], n_slots);
+        void* st = r.stream(a[11]);
+        return run(r, [&] {
+            return p_vector_block_tables((int32_t)B, lengths, added, page_rows, (int32_t*)table, (int32_t)width, stack, (int32_t)cap, n_free, new_lengths, new_n_free, first, start,
+                                         slots, n_slots, st);
+        });
+    });
+}
+METHOD(compact_q4) {                                    // shape, budget, K, V, ret_idx, apx_idx, cache, ret_slots, apx_slots, stream
+    return plain(n, 10, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        const vector_budget b = r.budget(a[1]);
+        const int64_t U = units_of(s), rows = U * b.n_tokens * s.head_dim;
+        void *k = r.sized(a[2], type_of(s), rows), *v = r.sized(a[3], type_of(s), rows);
+        const int32_t *ri = r.ints(a[4], U * b.n_ret), *ai = r.ints(a[5], U * b.n_apx);
+        const vector_q4_cache c = r.q4_cache(a[6], s, false);
+        const int32_t *rs = r.ints(a[7], s.batch * b.n_ret), *as = r.ints(a[8], s.batch * b.n_apx);
+        void* st = r.stream(a[9]);
+        return run(r, [&] { return p_vector_compact_q4(&s, &b, k, v, ri, ai, &c, rs, as, st); });
+    });
+}
+METHOD(append_q4) {                                     // shape, cache, k_new, v_new, row_start, slots, pos, stream
+    return plain(n, 8, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        const vector_q4_cache c = r.q4_cache(a[1], s, false);
+        const int64_t rows = units_of(s) * s.head_dim;
+        void *k = r.sized(a[2], type_of(s), rows), *v = r.sized(a[3], type_of(s), rows);
+        const int32_t *start = r.optional_ints(a[4], (int64_t)s.batch + 1), *slots = (const int32_t*)r.device(a[5], at::kInt), *pos = r.optional_ints(a[6], s.batch);
+        const int64_t n_slots = r.plain ? r.tensor(a[5])->numel() : 0;
+        void* st = r.stream(a[7]);
+        return run(r, [&] { return p_vector_append_q4(&s, &c, k, v, start, slots, n_slots, pos, st); });
+    });
+}
+METHOD(read_q4) {                                       // shape, cache, ret_slots, ret_k, ret_v, apx_slots, apx_k, stream
+    return plain(n, 8, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        const vector_q4_cache c = r.q4_cache(a[1], s, false);
+        if (!r.need(s.batch > 0)) return 0L;
+        const int64_t n_ret = r.numel(a[2]) / s.batch, n_apx = r.numel(a[5]) / s.batch, d = units_of(s) * s.head_dim;
+        const int32_t *rs = r.ints(a[2], s.batch * n_ret), *as = r.ints(a[5], s.batch * n_apx);
+        void *rk = r.sized(a[3], type_of(s), n_ret * d), *rv = r.sized(a[4], type_of(s), n_ret * d), *ak = r.sized(a[6], type_of(s), n_apx * d);
+        void* st = r.stream(a[7]);
+        return run(r, [&] { return p_vector_read_q4(&s, &c, rs, n_ret, rk, rv, as, n_apx, ak, st); });
+    });
+}
+METHOD(decode_attn_q4) {                                // shape, q, cache, W, out, ws, stream
+    return plain(n, 7, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        if (!r.need(s.n_kv_heads > 0)) return 0L;
+        const int64_t rows = units_of(s) * (s.n_q_heads / s.n_kv_heads) * s.head_dim;
+        void* q = r.sized(a[1], type_of(s), rows);
+        const vector_q4_cache c = r.q4_cache(a[2], s, true);
+        void* W = r.sized(a[3], type_of(s), (int64_t)s.n_layers * s.n_kv_heads * s.head_dim * s.head_dim);
+        const Out out = r.output(a[4]);
+        r.need(r.numel(a[4]) >= rows);
+        const Workspace w = r.workspace(a[5]);
+        void* st = r.stream(a[6]);
+        return run(r, [&] { return p_vector_decode_attn_q4(&s, q, &c, W, out.p, out.type, w.p, w.n, st); });
+    });
+}
+// The library's entry points, by the handle of the library that ctypes has loaded, and the classes of the structs.
 METHOD(bind) {
-    if (n != 4 || !PyLong_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2]) || !PyType_Check(a[3])) {
-        PyErr_SetString(PyExc_TypeError, "bind(handle, Shape, Budget, Cache)");
+    if (n != 5 || !PyLong_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2]) || !PyType_Check(a[3]) || !PyType_Check(a[4])) {
+        PyErr_SetString(PyExc_TypeError, "bind(handle, Shape, Budget, Cache, Q4Cache)");
         return nullptr;
     }
     void* handle = PyLong_AsVoidPtr(a[0]);
@@ -334,13 +457,15 @@ METHOD(bind) {
     p_##name = (decltype(p_##name))dlsym(handle, #name);                                                          \
     if (!p_##name) { PyErr_SetString(PyExc_ImportError, "libvector.so does not export " #name); return nullptr; }
     ENTRY_POINTS(RESOLVE)
-    if (!shape_class.set(a[1], "_p", "torch_dtype") || !budget_class.set(a[2], "_p") || !cache_class.set(a[3], "_p")) return nullptr;
+    if (!shape_class.set(a[1], "_p", "torch_dtype") || !budget_class.set(a[2], "_p") || !cache_class.set(a[3], "_p") || !q4_cache_class.set(a[4], "_p"))
+        return nullptr;
     Py_RETURN_NONE;
 }
 
 #define ROW(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ROW(bind), ROW(score), ROW(route), ROW(route_layer), ROW(compact), ROW(compact_layer), ROW(append), ROW(append_rows),
-                         ROW(decode_attn), ROW(decode_attn_layer), ROW(decode_attn_static), {nullptr, nullptr, 0, nullptr}};
+                         ROW(decode_attn), ROW(decode_attn_layer), ROW(decode_attn_static), ROW(block_tables), ROW(compact_q4), ROW(append_q4),
+                         ROW(read_q4), ROW(decode_attn_q4), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
