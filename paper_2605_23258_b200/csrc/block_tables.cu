@@ -2,8 +2,10 @@
 // requests' lengths and changes.  Everything is a prefix sum over the requests: pages released (pushed on the stack of free pages in the
 // requests' order), pages wanted (popped in that order) and rows added.  So no answer depends on the order in which threads run.
 //
-// What bounds a step of a batch is latency: one block does all of it, a thread a request, and writes the few slots too.  An
-// admission has millions of slots, 4 bytes each: a second kernel writes them, over all multiprocessors.
+// What bounds a step of a batch is latency: one block does all of it, a thread a request.  Where prompts are admitted there are many pages and
+// slots to write: blocks on all multiprocessors, each of which sums up the requests for itself and takes a part of the pages and slots; a page that a
+// request releases and another one takes in the same call is looked up where it was, so that no block waits for another one.  720000 slots
+// and 15000 pages of 512 requests: 12 us, with one block for the pages and a second kernel for the slots 22.  More than 1024 requests: one block moves the pages, a second kernel writes the slots.
 #include "common.cuh"
 #include "internal.h"
 
@@ -11,7 +13,7 @@ namespace vec {
 namespace bt {
 
 constexpr int THREADS = 1024, SLOT_THREADS = 256, SLOTS_PER_WARP = 128;
-constexpr int FEW_SLOTS = 4096;                 // slots that the first kernel writes itself, of at most THREADS requests
+constexpr int BLOCK_SLOTS = THREADS;            // slots that a block of block_tables_batch is there for, while there are multiprocessors
 
 struct Args {
     const int32_t *lengths, *added;
@@ -99,11 +101,11 @@ __device__ __forceinline__ void move_pages(const Args& a, int b0, int n, int tot
 }
 
 __global__ void __launch_bounds__(THREADS)
-block_tables_plan(Args a, int with_slots) {
+block_tables_plan(Args a) {
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     __shared__ int64_t warps[32];
-    __shared__ int32_t starts[THREADS], first[THREADS], olds[THREADS], news[THREADS];
+    __shared__ int32_t starts[THREADS], first[THREADS];
     const int t = threadIdx.x;
     int64_t height = min(max((int64_t)a.n_free[0], (int64_t)0), (int64_t)a.cap_free);
 
@@ -152,22 +154,106 @@ block_tables_plan(Args a, int with_slots) {
             a.first_row[b] = (int32_t)c.old_rows;
             a.row_start[b] = s;
             a.new_lengths[b] = rows;
-            if (with_slots) { starts[t] = s; olds[t] = (int32_t)c.old_rows; news[t] = rows; }
         }
     }
     if (t == 0) {
         a.row_start[a.batch] = (int32_t)min(added, (int64_t)0x7fffffff);
         a.new_n_free[0] = (int32_t)(height - min(needed, height));
     }
-    if (!with_slots) return;                                     // with them the requests are one round's
-    __syncthreads();
-    for (int64_t k = t; k < a.n_slots; k += THREADS) {
-        int32_t slot = -1;
-        if (k < added) {
-            const int b = request_of(starts, 0, a.batch, k);
-            slot = slot_of_row(a, b, olds[b] + (k - starts[b]), news[b]);
+}
+
+// At most THREADS requests, a thread a request in every block.  Blocks take parts of the pages and slots; `small` outputs, one number a request, are
+// written by the first block, in a launch of their own (parts = 0) where other blocks may still read what they overwrite.
+__global__ void __launch_bounds__(THREADS)
+block_tables_batch(Args a, int parts, int small) {
+    asm volatile("griddepcontrol.wait;\n" ::: "memory");
+    asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
+    __shared__ int64_t warps[32];
+    __shared__ int32_t row_start[THREADS], need_start[THREADS], back_start[THREADS], olds[THREADS], news[THREADS], haves[THREADS], wants[THREADS];
+    const int t = threadIdx.x;
+    const int64_t n_free = min(max((int64_t)a.n_free[0], (int64_t)0), (int64_t)a.cap_free);
+    Change c = {};
+    int grow = 0;
+    if (t < a.batch) { c = change_of(a, t); grow = a.added[t]; }
+    const int back = max(c.have - c.want, 0), need = max(c.want - c.have, 0);
+    int64_t total, backs = 0, before_back = 0;
+    // rows and pages wanted in one sum: pages are no more than rows, and rows below 2^31
+    const int64_t both = scan(((int64_t)max(grow, 0) << 32) | (uint32_t)need, warps, total);
+    const int64_t rows = total >> 32, needs = (int64_t)(uint32_t)total, start = both >> 32, before = (int64_t)(uint32_t)both;
+    if (__syncthreads_or(back > 0)) before_back = scan(back, warps, backs);
+    const int64_t height = min(n_free + backs, (int64_t)a.cap_free), pops = min(needs, height), pushes = height - n_free;
+    const int got = (int)min((int64_t)need, max(height - before, (int64_t)0));
+    const int32_t now = (int32_t)(grow > 0 ? min(c.rows, (int64_t)(c.have + got) * a.page_rows) : c.rows);
+    if (small && blockIdx.x == 0) {
+        if (t < a.batch) {
+            a.first_row[t] = (int32_t)c.old_rows;
+            a.row_start[t] = (int32_t)start;
+            a.new_lengths[t] = now;
         }
-        a.slots[k] = slot;
+        if (t == 0) {
+            a.row_start[a.batch] = (int32_t)rows;
+            a.new_n_free[0] = (int32_t)(height - pops);
+        }
+    }
+    if (!parts) return;
+    row_start[t] = (int32_t)start; need_start[t] = (int32_t)before; back_start[t] = (int32_t)before_back;
+    olds[t] = (int32_t)c.old_rows; news[t] = now; haves[t] = c.have; wants[t] = c.want;
+    __syncthreads();
+    auto released = [&](int64_t e) {                             // the e-th released page
+        const int k = request_of(back_start, 0, a.batch, e);
+        return a.table[(size_t)k * a.width + wants[k] + (e - back_start[k])];
+    };
+    auto taken = [&](int64_t e) {                                // the e-th page that is taken from the stack
+        const int64_t at = height - 1 - e;
+        return at >= n_free ? released(at - n_free) : a.stack[at];
+    };
+    // few pages and few slots are different warps' work
+    const int64_t i0 = (int64_t)blockIdx.x * THREADS + t, step = (int64_t)gridDim.x * THREADS, i1 = step - 1 - i0;
+    for (int64_t e = i1; e < pops; e += step) {
+        const int k = request_of(need_start, 0, a.batch, e);
+        a.table[(size_t)k * a.width + haves[k] + (e - need_start[k])] = taken(e);
+    }
+    for (int64_t e = i1; e < pushes; e += step) a.stack[n_free + e] = released(e);
+    if (a.n_slots <= step) {                                     // a slot a thread
+        if (i0 >= a.n_slots) return;
+        int32_t slot = -1;
+        if (i0 < rows) {
+            const int b = request_of(row_start, 0, a.batch, i0);
+            const int64_t row = olds[b] + (i0 - row_start[b]);
+            if (row < news[b]) {                                 // else no page was left for it
+                const int64_t j = (uint32_t)row / (uint32_t)a.page_rows;
+                slot = slot_of(j < haves[b] ? a.table[(size_t)b * a.width + j] : taken(need_start[b] + (j - haves[b])), row, a.page_rows);
+            }
+        }
+        a.slots[i0] = slot;
+        return;
+    }
+    const bool wide = ((uintptr_t)a.slots & 15) == 0;
+    for (int64_t k0 = 4 * i0; k0 < a.n_slots; k0 += 4 * step) {
+        int32_t slot[4] = {-1, -1, -1, -1};
+        if (k0 < rows) {
+            int b = request_of(row_start, 0, a.batch, k0);
+            int32_t page = -1;
+            int64_t index = -1;                                  // of the page at hand within its request
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int64_t k = k0 + i;
+                if (k >= rows) break;
+                if (b + 1 < a.batch && row_start[b + 1] <= k) { b = request_of(row_start, b + 1, a.batch, k); index = -1; }
+                const int64_t row = olds[b] + (k - row_start[b]);
+                if (row >= news[b]) continue;
+                const int64_t j = (uint32_t)row / (uint32_t)a.page_rows;
+                if (j != index) { page = j < haves[b] ? a.table[(size_t)b * a.width + j] : taken(need_start[b] + (j - haves[b])); index = j; }
+                slot[i] = slot_of(page, row, a.page_rows);
+            }
+        }
+        if (wide && k0 + 4 <= a.n_slots) {
+            *reinterpret_cast<int4*>(a.slots + k0) = make_int4(slot[0], slot[1], slot[2], slot[3]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k0 + i < a.n_slots) a.slots[k0 + i] = slot[i];
+        }
     }
 }
 
@@ -224,10 +310,18 @@ extern "C" vector_status vector_block_tables(int32_t batch, const int32_t* lengt
         (int64_t)width * page_rows > 0x7fffffffLL)
         return VECTOR_ERR_SHAPE;
     const bt::Args a = {lengths, added, new_lengths, table, free_pages, new_n_free, first_row, row_start, slots, n_free, n_slots, batch, page_rows, width, cap_free};
-    const bool few = n_slots <= bt::FEW_SLOTS && batch <= bt::THREADS;
     cudaStream_t st = (cudaStream_t)stream;
-    VEC_CUDA_CHECK(launch_maybe_dependent(true, bt::block_tables_plan, dim3(1), dim3(bt::THREADS), 0, st, a, few ? 1 : 0));
-    if (few || n_slots == 0) return VECTOR_OK;
+    if (batch <= bt::THREADS) {
+        const int64_t blocks = (n_slots + bt::BLOCK_SLOTS - 1) / bt::BLOCK_SLOTS, most = sm_count();
+        const int grid = (int)(blocks < 1 ? 1 : blocks > most ? most : blocks);
+        // other blocks read the lengths and the stack's height as they were
+        const bool apart = grid > 1 && (new_lengths == lengths || new_n_free == n_free);
+        VEC_CUDA_CHECK(launch_maybe_dependent(true, bt::block_tables_batch, dim3(grid), dim3(bt::THREADS), 0, st, a, 1, apart ? 0 : 1));
+        if (apart) VEC_CUDA_CHECK(launch_maybe_dependent(true, bt::block_tables_batch, dim3(1), dim3(bt::THREADS), 0, st, a, 0, 1));
+        return VECTOR_OK;
+    }
+    VEC_CUDA_CHECK(launch_maybe_dependent(true, bt::block_tables_plan, dim3(1), dim3(bt::THREADS), 0, st, a));
+    if (n_slots == 0) return VECTOR_OK;
     const int64_t per_block = (int64_t)bt::SLOT_THREADS / 32 * bt::SLOTS_PER_WARP;
     VEC_CUDA_CHECK(launch_maybe_dependent(true, bt::block_tables_slots, dim3((unsigned)((n_slots + per_block - 1) / per_block)), dim3(bt::SLOT_THREADS), 0, st, a));
     return VECTOR_OK;

@@ -70,15 +70,9 @@ __device__ __forceinline__ int tile_from(int64_t r, int nr) {
     return r <= (int64_t)COST_RET * nr ? (int)((r + COST_RET - 1) / COST_RET) : nr + (int)((r - (int64_t)COST_RET * nr + COST_APX - 1) / COST_APX);
 }
 
-#ifndef DQ4_W
-#define DQ4_W 12
-#endif
-#ifndef DQ4_E
-#define DQ4_E 3
-#endif
 template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
-    static constexpr int WARPS = EXACT || ROPE ? 8 : DQ4_W;
-    static constexpr int ENTRIES = EXACT || ROPE ? 4 : DQ4_E;          // of a warp's ring, a tile each
+    static constexpr int WARPS = EXACT && D == 128 ? 8 : 12;
+    static constexpr int ENTRIES = WARPS == 12 ? 3 : 4;                // of a warp's ring, a tile each
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int POS_AT = q4::Row<D>::TILE;                    // of a key-only tile's positions, within an entry
     static constexpr int ENTRY_BYTES = q4::Row<D>::TILE + (ROPE ? 4 * q4::ROWS : 0);
@@ -108,6 +102,11 @@ __device__ __forceinline__ uint32_t mul_h2(uint32_t a, uint32_t b) {
 __device__ __forceinline__ uint32_t fma_h2(uint32_t a, uint32_t b, uint32_t c) {
     uint32_t r;
     asm("fma.rn.f16x2 %0, %1, %2, %3;\n" : "=r"(r) : "r"(a), "r"(b), "r"(c));
+    return r;
+}
+__device__ __forceinline__ uint32_t neg_h2(uint32_t a) {
+    uint32_t r;
+    asm("neg.f16x2 %0, %1;\n" : "=r"(r) : "r"(a));
     return r;
 }
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
@@ -167,6 +166,12 @@ struct Runs {
 enum Kind { KEYS, VALUES, KEY_ONLY };
 struct Entry { int unit, rows, kind, first; };
 
+// Sine and cosine of an angle in 2^-32 turns, by its upper 23 bits (8e-7): they become a number in [1, 2) and that a multiple of 2 pi
+// about zero, without a conversion from integers, which would wait for the unit that the sine and the cosine keep busy.
+__device__ __forceinline__ void turn_cos_sin(uint32_t angle, float& cs, float& sn) {
+    const float turns = __uint_as_float((angle >> 9) ^ 0x3fc00000u);         // 1 + (angle + half a turn) modulo a turn
+    __sincosf(fmaf(turns, 6.283185307179586f, -9.42477796076938f), &sn, &cs);
+}
 // N neighbouring numbers at a multiple of 16 bytes.
 template <int N> __device__ __forceinline__ void load_run(const float* p, float* x) {
 #pragma unroll
@@ -195,7 +200,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     __shared__ __align__(8) uint64_t full[WARPS][ENTRIES];
     __shared__ Entry entries[WARPS][ENTRIES];
     __shared__ int64_t sums[WARPS];
-    __shared__ uint32_t phase32[ROPE ? D / 2 : 1];
+    __shared__ __align__(8) uint32_t phase32[ROPE ? D / 2 : 1];
     __shared__ RopePhase phase64[ROPE && EXACT ? D / 2 : 1];
     int64_t* prefix = reinterpret_cast<int64_t*>(smem + C::SMEM_BYTES);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
@@ -519,16 +524,18 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 logits(x, S[0]);
                 weigh(S, entry.rows - row0, ph, pl);
                 if constexpr (ROPE) {
+                    int32_t pos[2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const uint32_t pos = (uint32_t)reinterpret_cast<const int32_t*>(tile + C::POS_AT)[row0 + 8 * h + gid];
+                    for (int h = 0; h < 2; ++h) pos[h] = reinterpret_cast<const int32_t*>(tile + C::POS_AT)[row0 + 8 * h + gid];
 #pragma unroll
-                        for (int j = 0; j < C::PAIRS / 2; ++j) {
-                            const int ch = tig * (D / 8) + 2 * j;
+                    for (int j = 0; j < C::PAIRS / 2; ++j) {
+                        const int ch = tig * (D / 8) + 2 * j;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
                             uint32_t &u = x[h][j], &v = x[h][C::PAIRS / 2 + j];
                             if constexpr (EXACT) {
                                 uint64_t cs, sn;
-                                rope_cos_sin2(rope_angle((int32_t)pos, phase64[ch]), rope_angle((int32_t)pos, phase64[ch + 1]), cs, sn);
+                                rope_cos_sin2(rope_angle(pos[h], phase64[ch]), rope_angle(pos[h], phase64[ch + 1]), cs, sn);
                                 const float2 uf = unpack_h2(u), vf = unpack_h2(v);
                                 const uint64_t u2 = tc::pack2(uf.x, uf.y), v2 = tc::pack2(vf.x, vf.y);
                                 auto parts = [](uint64_t z, uint32_t& hi, uint32_t& low) {
@@ -541,12 +548,13 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                                 parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
                                 parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);
                             } else {
+                                const uint2 ph2 = *reinterpret_cast<const uint2*>(&phase32[ch]);
                                 float c0, s0, c1, s1;
-                                rope_phase32_cos_sin(pos, phase32[ch], c0, s0);
-                                rope_phase32_cos_sin(pos, phase32[ch + 1], c1, s1);
+                                turn_cos_sin((uint32_t)pos[h] * ph2.x, c0, s0);
+                                turn_cos_sin((uint32_t)pos[h] * ph2.y, c1, s1);
                                 const uint32_t cs = pack_h2(c0, c1), sn = pack_h2(s0, s1), a = u, b = v;
                                 u = fma_h2(a, cs, mul_h2(b, sn));
-                                v = fma_h2(b, cs, mul_h2(a ^ 0x80008000u, sn));
+                                v = fma_h2(neg_h2(a), sn, mul_h2(b, cs));
                             }
                         }
                     }
