@@ -27,13 +27,13 @@ struct Call {
         if (!fault) return VECTOR_ERR_CUDA;
         RopePhases ph = {};
         if (ROPE) rope_phases(dm.theta, D, &ph);
-        VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::SMEM_BYTES + (size_t)(c.batch + 1) * 8, st, (const T*)q, c, dm.g,
+        VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::SMEM_BYTES + (size_t)(c.batch + 1) * 8, st, (const T*)q, c, dm.g, C::COST,
                                               dm.scale * 1.4426950408889634f, ws, fault, ph));
         const int workers = sm_count() * C::WARPS;
-        return out_dtype == VECTOR_F32 ? merge<T, D, float>(workers) : merge<T, D, __nv_bfloat16>(workers);
+        return out_dtype == VECTOR_F32 ? merge<T, D, float>(C::COST, workers) : merge<T, D, __nv_bfloat16>(C::COST, workers);
     }
-    template <typename T, int D, typename TO> vector_status merge(int workers) const {
-        VEC_CUDA_CHECK(launch_maybe_dependent(true, decode_q4_merge<T, D, TO>, dim3(dm.U), dim3(MERGE_THREADS), 0, st, (const unsigned char*)ws, c, dm.g,
+    template <typename T, int D, typename TO> vector_status merge(Costs cost, int workers) const {
+        VEC_CUDA_CHECK(launch_maybe_dependent(true, decode_q4_merge<T, D, TO>, dim3(dm.U), dim3(MERGE_THREADS), 0, st, (const unsigned char*)ws, c, dm.g, cost,
                                               workers, (const T*)W, (TO*)out));
         return VECTOR_OK;
     }

@@ -34,11 +34,11 @@ namespace vec {
 namespace dq4 {
 
 constexpr int MAX_BATCH = VECTOR_Q4_MAX_BATCH;
-#ifndef DQ4_CR
-#define DQ4_CR 4
-#define DQ4_CA 3
-#endif
-constexpr int COST_RET = DQ4_CR, COST_APX = DQ4_CA, COST_MOST = DQ4_CR;      // of a tile
+// What a tile of either tier costs a worker, in small numbers.
+struct Costs {
+    int ret, apx;
+    __host__ __device__ int most() const { return ret > apx ? ret : apx; }
+};
 constexpr float SLACK = 8.f;
 
 struct Cache {
@@ -61,13 +61,15 @@ __host__ __device__ inline int tier_floats(int g, int d) { return even_heads(g) 
 struct Deal {
     int64_t X;
     int workers;
-    __device__ __forceinline__ Deal(int64_t x, int most) : X(x), workers((int)max(min((int64_t)most, x / COST_MOST), (int64_t)1)) {}
+    __device__ __forceinline__ Deal(int64_t x, int workers_at_most, Costs cost)
+        : X(x), workers((int)max(min((int64_t)workers_at_most, x / cost.most()), (int64_t)1)) {}
     __device__ __forceinline__ int64_t begin(int w) const { return X * w / workers; }
     __device__ __forceinline__ int owner(int64_t x) const { return (int)(((x + 1) * workers - 1) / X); }
 };
 // First tile of a unit that begins at r or later, r counted from the unit's beginning.
-__device__ __forceinline__ int tile_from(int64_t r, int nr) {
-    return r <= (int64_t)COST_RET * nr ? (int)((r + COST_RET - 1) / COST_RET) : nr + (int)((r - (int64_t)COST_RET * nr + COST_APX - 1) / COST_APX);
+__device__ __forceinline__ int tile_from(int64_t r, int nr, Costs cost) {
+    const int64_t ret = (int64_t)cost.ret * nr;
+    return r <= ret ? (int)((r + cost.ret - 1) / cost.ret) : nr + (int)((r - ret + cost.apx - 1) / cost.apx);
 }
 
 template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
@@ -80,6 +82,7 @@ template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
+    static constexpr Costs COST = ROPE ? Costs{2, 3} : Costs{4, 3};
 };
 
 // Not volatile, like the transposes: the compiler may move them past one another, so that one's operands are on their way during the next.
@@ -118,6 +121,7 @@ __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(
 
 // A worker's way through the sequence of tiles, as runs: tiles of one tier of one unit.
 struct Runs {
+    Costs cost;
     int64_t left;                               // cost up to the end of the worker's range
     int b, lh, n_ret, n_apx;                    // sequence, (layer, KV head), rows
     int apx, p, count;                          // the run: tier, first tile of it, tiles
@@ -138,9 +142,10 @@ struct Runs {
         }
         apx = t >= nr;
         p = apx ? t - nr : t;
-        const int64_t in_range = apx ? (left + COST_APX - 1) / COST_APX : (left + COST_RET - 1) / COST_RET;
+        const int each = apx ? cost.apx : cost.ret;
+        const int64_t in_range = (left + each - 1) / each;
         count = b < c.batch ? (int)max(min((int64_t)((apx ? tiles_of(n_apx) : nr) - p), in_range), (int64_t)0) : 0;
-        left -= (int64_t)count * (apx ? COST_APX : COST_RET);
+        left -= (int64_t)count * each;
     }
     __device__ __forceinline__ void next(const Cache& c, const int64_t* prefix) { run(c, prefix, p + count + (apx ? tiles_of(n_ret) : 0)); }
     // The first run of the costs [x, end).
@@ -156,8 +161,8 @@ struct Runs {
         const int64_t unit = (prefix[b + 1] - prefix[b]) / c.LH;
         lh = (int)((x - prefix[b]) / unit);
         const int64_t r = x - prefix[b] - lh * unit;
-        const int nr = tiles_of(n_ret), t = tile_from(r, nr);
-        left = end - x - ((t < nr ? (int64_t)COST_RET * t : (int64_t)COST_RET * nr + (int64_t)COST_APX * (t - nr)) - r);
+        const int nr = tiles_of(n_ret), t = tile_from(r, nr, cost);
+        left = end - x - ((int64_t)cost.ret * min(t, nr) + (int64_t)cost.apx * max(t - nr, 0) - r);
         run(c, prefix, t);
     }
 };
@@ -192,7 +197,7 @@ template <int N> __device__ __forceinline__ void load_run(const __nv_bfloat16* p
 
 template <typename T, int D, bool ROPE, bool EXACT>
 __global__ void __launch_bounds__(Cfg<T, D, ROPE, EXACT>::THREADS, 1)
-decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* ws, int* fault, RopePhases phases) {
+decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsigned char* ws, int* fault, RopePhases phases) {
     using C = Cfg<T, D, ROPE, EXACT>;
     using R = q4::Row<D>;
     constexpr int WARPS = C::WARPS, ENTRIES = C::ENTRIES;
@@ -223,7 +228,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         const int b = b0 + threadIdx.x;
         int64_t x = 0;
         if (b < c.batch)
-            x = (int64_t)c.LH * (COST_RET * tiles_of(rows_of(c.ret_len, b, c.ret_width)) + COST_APX * tiles_of(rows_of(c.apx_len, b, c.apx_width)));
+            x = (int64_t)c.LH * ((int64_t)cost.ret * tiles_of(rows_of(c.ret_len, b, c.ret_width)) + (int64_t)cost.apx * tiles_of(rows_of(c.apx_len, b, c.apx_width)));
         int64_t s = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -243,7 +248,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     __syncthreads();
     if (blockIdx.x == 0)
         for (int b = threadIdx.x; b <= c.batch; b += C::THREADS) reinterpret_cast<int64_t*>(ws)[b] = prefix[b];
-    const Deal deal(carry, gridDim.x * WARPS);
+    const Deal deal(carry, gridDim.x * WARPS, cost);
     const int worker = wid * gridDim.x + blockIdx.x;        // neighbours in the sequence on different multiprocessors
     if (carry == 0 || worker >= deal.workers) return;
 
@@ -254,6 +259,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
 
     // ---- the producing side, ENTRIES ahead: `run` is where it is, `k` tiles of it are on their way, and lane l has the page of tile l of 32
     Runs run;
+    run.cost = cost;
     run.find(c, prefix, deal.begin(worker), deal.begin(worker + 1));
     int k = 0, page = -1, values = 0;
     auto issue = [&](int s) {
@@ -607,7 +613,7 @@ template <int D> struct MapRows<float, D> {
 // The records of a unit into its outputs.
 template <typename T, int D, typename TO>
 __global__ void __launch_bounds__(MERGE_THREADS)
-decode_q4_merge(const unsigned char* ws, Cache c, int g, int most_workers, const T* W, TO* __restrict__ out) {
+decode_q4_merge(const unsigned char* ws, Cache c, int g, Costs cost, int most_workers, const T* W, TO* __restrict__ out) {
     constexpr int NW = MERGE_THREADS / 32, ROWS_W = 16;
     __shared__ __align__(16) float val[8][D + 4], keys[8][D + 4];
     __shared__ float ref[8], inv[8], fac[2][8][MERGE_CHUNK];
@@ -627,11 +633,11 @@ decode_q4_merge(const unsigned char* ws, Cache c, int g, int most_workers, const
         for (int e = threadIdx.x; e < g * D; e += MERGE_THREADS) store_out(o + e, 0.f);
         return;
     }
-    const int64_t cost = (int64_t)COST_RET * nr + (int64_t)COST_APX * na, from = p0 + lh * cost;
-    const Deal deal(X, most_workers);
+    const int64_t unit_cost = (int64_t)cost.ret * nr + (int64_t)cost.apx * na, from = p0 + lh * unit_cost;
+    const Deal deal(X, most_workers, cost);
     const int w0 = deal.owner(from);
-    int last = deal.owner(from + cost - 1);
-    if (last > w0 && tile_from(deal.begin(last) - from, nr) >= nr + na) --last;       // its range begins within the unit's last tile
+    int last = deal.owner(from + unit_cost - 1);
+    if (last > w0 && tile_from(deal.begin(last) - from, nr, cost) >= nr + na) --last;       // its range begins within the unit's last tile
     const int pieces = last - w0 + 1;                                 // the unit's own record, then those of workers w0 + 1 ..
     const float *own = records + (size_t)u * 2 * tier, *others = records + (size_t)(units + w0) * 2 * tier;
     auto piece = [&](int i) { return i == 0 ? own : others + (size_t)i * 2 * tier; };
