@@ -82,6 +82,7 @@ template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
+    static constexpr int N_APX = ROPE ? 1 : 2;                         // key-only rows of a step, in sixteens
     static constexpr Costs COST = ROPE ? Costs{2, 3} : Costs{4, 3};
 };
 
@@ -440,6 +441,44 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
         L[0] += sum[0]; L[1] += sum[1];
     };
 
+    // The 16 rows at row0 turned back by their positions; lo: second parts.
+    auto turn_back = [&](const unsigned char* tile, int row0, uint32_t (&x)[2][C::PAIRS], auto& lo) {
+        int32_t pos[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) pos[h] = reinterpret_cast<const int32_t*>(tile + C::POS_AT)[row0 + 8 * h + gid];
+#pragma unroll
+        for (int j = 0; j < C::PAIRS / 2; ++j) {
+            const int ch = tig * (D / 8) + 2 * j;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                uint32_t &u = x[h][j], &v = x[h][C::PAIRS / 2 + j];
+                if constexpr (EXACT) {
+                    uint64_t cs, sn;
+                    rope_cos_sin2(rope_angle(pos[h], phase64[ch]), rope_angle(pos[h], phase64[ch + 1]), cs, sn);
+                    const float2 uf = unpack_h2(u), vf = unpack_h2(v);
+                    const uint64_t u2 = tc::pack2(uf.x, uf.y), v2 = tc::pack2(vf.x, vf.y);
+                    auto parts = [](uint64_t z, uint32_t& hi, uint32_t& low) {
+                        float a, b;
+                        tc::unpack2(z, a, b);
+                        hi = pack_h2(a, b);
+                        const float2 f = unpack_h2(hi);
+                        low = pack_h2(a - f.x, b - f.y);
+                    };
+                    parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
+                    parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);
+                } else {
+                    const uint2 ph2 = *reinterpret_cast<const uint2*>(&phase32[ch]);
+                    float c0, s0, c1, s1;
+                    turn_cos_sin((uint32_t)pos[h] * ph2.x, c0, s0);
+                    turn_cos_sin((uint32_t)pos[h] * ph2.y, c1, s1);
+                    const uint32_t cs = pack_h2(c0, c1), sn = pack_h2(s0, s1), a = u, b = v;
+                    u = fma_h2(a, cs, mul_h2(b, sn));
+                    v = fma_h2(neg_h2(a), sn, mul_h2(b, cs));
+                }
+            }
+        }
+    };
+
     int unit = -1, apx = 0, wrote = 0, slot_rec = 0;
     // The state of a tier to its record; an empty one's sums are not read.
     auto put_tier = [&](int tier, bool empty) {
@@ -521,51 +560,22 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
             }
             release(of_keys);
         } else {
+            constexpr int N = C::N_APX;
             if (entry.rows < q4::ROWS) blank(tile, entry.rows);
 #pragma unroll 1
-            for (int row0 = 0; row0 < entry.rows; row0 += 16) {
-                uint32_t x[2][C::PAIRS], ph[1][2], pl[1][2], lo[ROPE && EXACT ? 2 : 1][ROPE && EXACT ? C::PAIRS : 1];
-                float S[1][4];
-                load_rows(tile, row0, x);
-                logits(x, S[0]);
+            for (int row0 = 0; row0 < entry.rows; row0 += 16 * N) {
+                uint32_t x[N][2][C::PAIRS], ph[N][2], pl[N][2], lo[ROPE && EXACT ? N : 1][ROPE && EXACT ? 2 : 1][ROPE && EXACT ? C::PAIRS : 1];
+                float S[N][4];
+#pragma unroll
+                for (int i = 0; i < N; ++i) load_rows(tile, row0 + 16 * i, x[i]);
+#pragma unroll
+                for (int i = 0; i < N; ++i) logits(x[i], S[i]);
                 weigh(S, entry.rows - row0, ph, pl);
-                if constexpr (ROPE) {
-                    int32_t pos[2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) pos[h] = reinterpret_cast<const int32_t*>(tile + C::POS_AT)[row0 + 8 * h + gid];
-#pragma unroll
-                    for (int j = 0; j < C::PAIRS / 2; ++j) {
-                        const int ch = tig * (D / 8) + 2 * j;
-#pragma unroll
-                        for (int h = 0; h < 2; ++h) {
-                            uint32_t &u = x[h][j], &v = x[h][C::PAIRS / 2 + j];
-                            if constexpr (EXACT) {
-                                uint64_t cs, sn;
-                                rope_cos_sin2(rope_angle(pos[h], phase64[ch]), rope_angle(pos[h], phase64[ch + 1]), cs, sn);
-                                const float2 uf = unpack_h2(u), vf = unpack_h2(v);
-                                const uint64_t u2 = tc::pack2(uf.x, uf.y), v2 = tc::pack2(vf.x, vf.y);
-                                auto parts = [](uint64_t z, uint32_t& hi, uint32_t& low) {
-                                    float a, b;
-                                    tc::unpack2(z, a, b);
-                                    hi = pack_h2(a, b);
-                                    const float2 f = unpack_h2(hi);
-                                    low = pack_h2(a - f.x, b - f.y);
-                                };
-                                parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
-                                parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);
-                            } else {
-                                const uint2 ph2 = *reinterpret_cast<const uint2*>(&phase32[ch]);
-                                float c0, s0, c1, s1;
-                                turn_cos_sin((uint32_t)pos[h] * ph2.x, c0, s0);
-                                turn_cos_sin((uint32_t)pos[h] * ph2.y, c1, s1);
-                                const uint32_t cs = pack_h2(c0, c1), sn = pack_h2(s0, s1), a = u, b = v;
-                                u = fma_h2(a, cs, mul_h2(b, sn));
-                                v = fma_h2(neg_h2(a), sn, mul_h2(b, cs));
-                            }
-                        }
-                    }
+                for (int i = 0; i < N; ++i) {
+                    if constexpr (ROPE) turn_back(tile, row0 + 16 * i, x[i], lo[EXACT ? i : 0]);
+                    add_rows(x[i], ph[i], pl[i], lo[ROPE && EXACT ? i : 0], std::bool_constant<ROPE && EXACT>());
                 }
-                add_rows(x, ph[0], pl[0], lo, std::bool_constant<ROPE && EXACT>());
             }
         }
         release(at);

@@ -15,6 +15,7 @@
 #define VECTOR_Q4_CUH_
 
 #include "common.cuh"
+#include "tcgen05.cuh"
 #include "vector.h"
 
 namespace vec {
@@ -49,19 +50,45 @@ __device__ __forceinline__ uint32_t scale_code(float most) {
     return min(c, (uint32_t)SCALE_TOP);
 }
 
-// Two numbers to their codes, the first in the low nibble.
-__device__ __forceinline__ uint32_t to_codes(float lo, float hi) {
+// Eight numbers to their codes, the first in the lowest nibble.
+__device__ __forceinline__ uint32_t to_codes(const float (&q)[8]) {
     uint32_t r;
-    asm("{\n .reg .b8 b;\n cvt.rn.satfinite.e2m1x2.f32 b, %1, %2;\n cvt.u32.u8 %0, b;\n}\n" : "=r"(r) : "f"(hi), "f"(lo));
+    asm("{\n .reg .b8 a, b, c, d;\n cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n mov.b32 %0, {a, b, c, d};\n}\n"
+        : "=r"(r) : "f"(q[0]), "f"(q[1]), "f"(q[2]), "f"(q[3]), "f"(q[4]), "f"(q[5]), "f"(q[6]), "f"(q[7]));
     return r;
 }
-// x / s, by 1 / s, on the right side of every border between codes.  A border is t s, t of at most three significant bits.
-// bf16: x has eight bits and t s seven, so x is t s or at least 2^-7 / 1.875 of it away (2^-8 below); the quotient rounded to bf16
-// is then t where x = t s, and no border nor beyond one where it is not: half a step of bf16 is 2^-8 at most.
-__device__ __forceinline__ uint32_t quotient_codes(float a, float b, float, float inv, __nv_bfloat16) {
-    const __nv_bfloat162 v = __floats2bfloat162_rn(a * inv, b * inv);
-    const uint32_t u = *reinterpret_cast<const uint32_t*>(&v);
-    return to_codes(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u));
+// The quotients x / s are on the right side of every border between codes.  A border is t s, t of at most three significant bits.
+// bf16: x has eight bits and t s seven, so x is t s or at least 2^-8 of it away, which no rounding below crosses; and where x = t s the quotient has to be t: 1 / s enters in
+// two parts, so that what is left of x / s is under 2^-40 of it and the last rounding gives t.
+__device__ __forceinline__ uint2 encode_group(const uint4 (&v)[2], uint32_t& scale) {
+    uint32_t w[8] = {v[0].x, v[0].y, v[0].z, v[0].w, v[1].x, v[1].y, v[1].z, v[1].w};
+    uint32_t most = w[0] & 0x7fff7fffu;                                // magnitudes order like their bits, NaN above all
+#pragma unroll
+    for (int i = 1; i < 8; ++i) asm("max.u16x2 %0, %0, %1;\n" : "+r"(most) : "r"(w[i] & 0x7fff7fffu));
+    scale = scale_code(__uint_as_float(max(most << 16, most & 0xffff0000u)));
+    if (scale >= SCALE_TOP) {                                          // infinities count as the largest number
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t size = w[i] & 0x7fff7fffu;
+            asm("min.u16x2 %0, %0, %1;\n" : "+r"(size) : "r"(0x7f7f7f7fu));
+            w[i] = size | (w[i] & 0x80008000u);
+        }
+    }
+    const float s = scale_value(scale), inv = s > 0.f ? __frcp_rn(s) : 0.f, rest = fmaf(-inv, s, s > 0.f ? 1.f : 0.f) * inv;
+    const uint64_t inv2 = tc::pack2(inv, inv), rest2 = tc::pack2(rest, rest);
+    uint32_t codes[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        float q[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint64_t x = tc::pack2(__uint_as_float(w[4 * h + i] << 16), __uint_as_float(w[4 * h + i] & 0xffff0000u));
+            tc::unpack2(tc::fma2(x, inv2, tc::mul2(x, rest2)), q[2 * i], q[2 * i + 1]);
+        }
+        codes[h] = to_codes(q);
+    }
+    return make_uint2(codes[0], codes[1]);
 }
 // fp32: the quotient rounded to twelve bits (h s is exact then), moved by one unit in the last place to the side that what is left, x - h s, says.
 __device__ __forceinline__ float quotient_f32(float x, float s, float inv) {
@@ -70,26 +97,23 @@ __device__ __forceinline__ float quotient_f32(float x, float s, float inv) {
     const bool out = (__float_as_uint(left) ^ h) >> 31 == 0;           // away from zero
     return __uint_as_float(h + (left > 0.f || left < 0.f ? (out ? 1u : 0xffffffffu) : 0u));
 }
-__device__ __forceinline__ uint32_t quotient_codes(float a, float b, float s, float inv, float) {
-    return to_codes(quotient_f32(a, s, inv), quotient_f32(b, s, inv));
-}
-
-// 16 channels x to eight bytes of codes, in their order, and a scale.
-template <typename T>
-__device__ __forceinline__ uint2 encode_group(const float (&x)[16], uint32_t& scale) {
-    uint32_t most = 0;                                                 // magnitudes order like their bits, NaN above all
+__device__ __forceinline__ uint2 encode_group(const uint4 (&v)[4], uint32_t& scale) {
+    uint32_t x[16], most = 0;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+    for (int i = 0; i < 4; ++i) { x[4 * i] = v[i].x; x[4 * i + 1] = v[i].y; x[4 * i + 2] = v[i].z; x[4 * i + 3] = v[i].w; }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = max(most, x[i] & 0x7fffffffu);
     scale = scale_code(__uint_as_float(most));
     const float s = scale_value(scale), inv = s > 0.f ? __frcp_rn(s) : 0.f;
-    uint32_t w[2];
+    uint32_t codes[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        w[h] = 0;
+        float q[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[h] |= quotient_codes(x[8 * h + 2 * i], x[8 * h + 2 * i + 1], s, inv, T()) << (8 * i);
+        for (int i = 0; i < 8; ++i) q[i] = quotient_f32(__uint_as_float(x[8 * h + i]), s, inv);
+        codes[h] = to_codes(q);
     }
-    return make_uint2(w[0], w[1]);
+    return make_uint2(codes[0], codes[1]);
 }
 
 // The eight codes of a word as four fp16 pairs, before the scale.
