@@ -7,8 +7,8 @@ namespace dq4 {
 
 constexpr int MOST_WARPS = 16;          // of a streaming block, over all kernels
 
-static size_t ws_bytes_of(const Dims& dm, int batch) {
-    return prefix_bytes(batch) + ((size_t)dm.U + sm_count() * MOST_WARPS) * 2 * tier_floats(dm.g, dm.d) * 4;
+static size_t ws_bytes_of(const Dims& dm) {
+    return ends_bytes(dm.U) + ((size_t)dm.U + sm_count() * MOST_WARPS) * 2 * tier_floats(dm.g, dm.d) * 4;
 }
 
 struct Call {
@@ -29,13 +29,32 @@ struct Call {
         if (ROPE) rope_phases(dm.theta, D, &ph);
         VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::SMEM_BYTES + (size_t)(c.batch + 1) * 8, st, (const T*)q, c, dm.g, C::COST,
                                               dm.scale * 1.4426950408889634f, ws, fault, ph));
-        const int workers = sm_count() * C::WARPS;
-        return out_dtype == VECTOR_F32 ? merge<T, D, float>(C::COST, workers) : merge<T, D, __nv_bfloat16>(C::COST, workers);
+        return merge<T, D>();
     }
-    template <typename T, int D, typename TO> vector_status merge(Costs cost, int workers) const {
-        VEC_CUDA_CHECK(launch_maybe_dependent(true, decode_q4_merge<T, D, TO>, dim3(dm.U), dim3(MERGE_THREADS), 0, st, (const unsigned char*)ws, c, dm.g, cost,
-                                              workers, (const T*)W, (TO*)out));
+    template <typename T, int D, int HP, int THREADS> vector_status merge_by(int seqs) const {
+        auto kern = decode_q4_merge<T, D, HP, THREADS>;
+        constexpr int smem = MapTile<T, D>::BYTES;
+        static PerDeviceOnce once;
+        if (once.first()) {
+            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+            if (e != cudaSuccess) { once.undo(); VEC_CUDA_CHECK(e); }
+        }
+        VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3((unsigned)(dm.LH * ((c.batch + seqs - 1) / seqs))), dim3(THREADS), smem, st, (const unsigned char*)ws, c,
+                                              dm.g, seqs, (const T*)W, out, out_dtype == VECTOR_BF16 ? 1 : 0));
         return VECTOR_OK;
+    }
+    // A unit a multiprocessor: a large block a unit, since the records are many.  More: small blocks, and as many sequences for a fetched map as leave a round of blocks.
+    template <typename T, int D, int HP> vector_status merge_heads() const {
+        if (dm.U <= sm_count()) return merge_by<T, D, HP, MERGE_MOST>(1);
+#ifndef DQ4_S
+        const int resident = (sizeof(T) == 2 ? 4 : 3) * sm_count(), rounds = (dm.U + resident - 1) / resident;
+#else
+        const int rounds = DQ4_S;
+#endif
+        return merge_by<T, D, HP, MERGE_THREADS>(rounds < c.batch ? rounds : c.batch);
+    }
+    template <typename T, int D> vector_status merge() const {
+        return dm.g <= 2 ? merge_heads<T, D, 1>() : dm.g <= 4 ? merge_heads<T, D, 2>() : dm.g <= 6 ? merge_heads<T, D, 3>() : merge_heads<T, D, 4>();
     }
     template <typename T, int D> vector_status run() const {
         const bool exact = dm.dtype == VECTOR_F32 || out_dtype == VECTOR_F32;
@@ -53,7 +72,7 @@ using namespace vec;
 extern "C" size_t vector_decode_q4_workspace_bytes(const vector_shape* shape) {
     Dims dm;
     if (check_shape(shape, &dm) != VECTOR_OK) return 0;
-    return dq4::ws_bytes_of(dm, shape->batch);
+    return dq4::ws_bytes_of(dm);
 }
 
 extern "C" vector_status vector_decode_attn_q4(const vector_shape* shape, const void* q, const vector_q4_cache* cache, const void* W, void* out,
@@ -70,7 +89,7 @@ extern "C" vector_status vector_decode_attn_q4(const vector_shape* shape, const 
     if (cache->ret_width > 0 && (!cache->ret_table || !cache->ret_len)) return VECTOR_ERR_NULL;
     if (cache->apx_width > 0 && (!cache->apx_table || !cache->apx_len)) return VECTOR_ERR_NULL;
     if (dm.rope && cache->n_apx_pages > 0 && !cache->apx_pos) return VECTOR_ERR_NULL;
-    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < dq4::ws_bytes_of(dm, shape->batch)) return VECTOR_ERR_WORKSPACE;
+    if (!ws || ((uintptr_t)ws & 255) || ws_bytes < dq4::ws_bytes_of(dm)) return VECTOR_ERR_WORKSPACE;
     if (((uintptr_t)q | (uintptr_t)W | (uintptr_t)out | (uintptr_t)cache->apx_pos) & 15) return VECTOR_ERR_SHAPE;
     const dq4::Cache c = {(const unsigned char*)cache->ret_pages, (const unsigned char*)cache->apx_pages, cache->ret_table, cache->apx_table,
                           cache->ret_len, cache->apx_len, cache->apx_pos, cache->n_ret_pages, cache->n_apx_pages, cache->ret_width, cache->apx_width, dm.LH,

@@ -51,8 +51,8 @@ struct Cache {
 __device__ __forceinline__ int rows_of(const int32_t* len, int b, int width) { return width ? min(max(len[b], 0), width * q4::ROWS) : 0; }
 __device__ __forceinline__ int tiles_of(int rows) { return (rows + q4::ROWS - 1) / q4::ROWS; }
 
-// ---- workspace: prefix sums of the costs [batch + 1], then the records
-__host__ __device__ inline size_t prefix_bytes(int batch) { return (((size_t)batch + 1) * 8 + 255) & ~(size_t)255; }
+// ---- workspace: the first and the last worker of every unit that has tiles, then the records
+__host__ __device__ inline size_t ends_bytes(int units) { return ((size_t)units * 8 + 255) & ~(size_t)255; }
 // A record: for each tier [heads, rounded up to even][m, l] and the sums, in the order of the fragments.
 __host__ __device__ inline int even_heads(int g) { return (g + 1) & ~1; }
 __host__ __device__ inline int tier_floats(int g, int d) { return even_heads(g) * (d + 2); }
@@ -64,7 +64,6 @@ struct Deal {
     __device__ __forceinline__ Deal(int64_t x, int workers_at_most, Costs cost)
         : X(x), workers((int)max(min((int64_t)workers_at_most, x / cost.most()), (int64_t)1)) {}
     __device__ __forceinline__ int64_t begin(int w) const { return X * w / workers; }
-    __device__ __forceinline__ int owner(int64_t x) const { return (int)(((x + 1) * workers - 1) / X); }
 };
 // First tile of a unit that begins at r or later, r counted from the unit's beginning.
 __device__ __forceinline__ int tile_from(int64_t r, int nr, Costs cost) {
@@ -168,9 +167,9 @@ struct Runs {
     }
 };
 
-// What an entry of a ring holds, for its consumer: unit, rows that are there, whether it is the unit's first tile.
+// What an entry of a ring holds, for its consumer: unit, rows that are there, whether it is the unit's first (1) or last (2) tile.
 enum Kind { KEYS, VALUES, KEY_ONLY };
-struct Entry { int unit, rows, kind, first; };
+struct Entry { int unit, rows, kind, edge; };
 
 // Sine and cosine of an angle in 2^-32 turns, by its upper 23 bits (8e-7): they become a number in [1, 2) and that a multiple of 2 pi
 // about zero, without a conversion from integers, which would wait for the unit that the sine and the cosine keep busy.
@@ -247,14 +246,13 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
     }
     if (threadIdx.x == 0) prefix[c.batch] = carry;
     __syncthreads();
-    if (blockIdx.x == 0)
-        for (int b = threadIdx.x; b <= c.batch; b += C::THREADS) reinterpret_cast<int64_t*>(ws)[b] = prefix[b];
     const Deal deal(carry, gridDim.x * WARPS, cost);
     const int worker = wid * gridDim.x + blockIdx.x;        // neighbours in the sequence on different multiprocessors
     if (carry == 0 || worker >= deal.workers) return;
 
-    float* records = reinterpret_cast<float*>(ws + prefix_bytes(c.batch));
     const int rec = 2 * tier_floats(g, D), heads = even_heads(g), units = c.batch * c.LH;
+    int2* ends = reinterpret_cast<int2*>(ws);
+    float* records = reinterpret_cast<float*>(ws + ends_bytes(units));
     unsigned char* ring = smem + wid * ENTRIES * C::ENTRY_BYTES;
     const uint64_t policy = tma::policy_evict_first();
 
@@ -272,7 +270,8 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
             const int p = run.p + k;
             const size_t tile = (size_t)at * c.LH + run.lh;
             entries[wid][s] = Entry{run.b * c.LH + run.lh, there ? min((run.apx ? run.n_apx : run.n_ret) - p * q4::ROWS, (int)q4::ROWS) : 0,
-                                    run.apx ? KEY_ONLY : values ? VALUES : KEYS, p == 0 && (!run.apx || run.n_ret == 0)};
+                                    run.apx ? KEY_ONLY : values ? VALUES : KEYS,
+                                    (p == 0 && (!run.apx || run.n_ret == 0) ? 1 : 0) | (run.apx ? (p + 1) * q4::ROWS >= run.n_apx : run.n_apx == 0 && (p + 1) * q4::ROWS >= run.n_ret ? 1 : 0) << 1};
             uint64_t* bar = &full[wid][s];
             unsigned char* to = ring + s * C::ENTRY_BYTES;
             if (!there) {
@@ -525,7 +524,7 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
         if (entry.unit != unit) {
             leave_unit();
             unit = entry.unit; apx = tier; wrote = 0;
-            slot_rec = entry.first ? unit : units + worker;
+            slot_rec = entry.edge & 1 ? unit : units + worker;
             clear();
             load_queries(unit);
         } else if (tier != apx) {
@@ -533,6 +532,10 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
             wrote |= 1 << apx;
             apx = tier;
             clear();
+        }
+        if (lane == 0) {
+            if (entry.edge & 1) ends[unit].x = worker;
+            if (entry.edge & 2) ends[unit].y = worker;
         }
         unsigned char* tile = ring + at * C::ENTRY_BYTES;
         if (!tier) {
@@ -584,206 +587,194 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
     leave_unit();
 }
 
-constexpr int MERGE_THREADS = 256;
-constexpr int FEW_PIECES = 4;        // records of a unit that every thread weighs for itself
-constexpr int MERGE_CHUNK = 64;      // records weighed at a time where there are more
+// Threads of a merge block, which takes the records of a unit in groups of MERGE_THREADS, each a part of the records.
+constexpr int MERGE_THREADS = 256, MERGE_MOST = 1024;
+constexpr int MERGE_CHUNK = 64;      // records of a unit that are weighed at a time
 
-// The map's rows 16 w + gid and 16 w + gid + 8 as a thread holds them: channels 32 i + 8 tig .. + 7 of each.
-template <typename T, int D> struct MapRows;
-template <int D> struct MapRows<__nv_bfloat16, D> {
-    static constexpr int PARTS = 1;
-    uint4 w[2][D / 32];
-    __device__ __forceinline__ void load(const __nv_bfloat16* W, int tig) {
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < D / 32; ++i) w[h][i] = *reinterpret_cast<const uint4*>(W + h * 8 * D + 32 * i + 8 * tig);
+// The map in shared memory, its 16-byte pieces so that a fragment's rows do not meet in a bank: pieces of odd rows change places.
+template <typename T, int D> struct MapTile {
+    static constexpr int PIECES = D * sizeof(T) / 16, BYTES = D * PIECES * 16, FLIP = sizeof(T) == 2 ? 4 : 1, PARTS = sizeof(T) == 2 ? 1 : 3;
+    __device__ __forceinline__ static int at(int row, int piece) { return (row * PIECES + (piece ^ ((row & 1) * FLIP))) * 16; }
+    template <int THREADS> __device__ __forceinline__ static void request(unsigned char* to, const T* W) {
+        for (int i = threadIdx.x; i < D * PIECES; i += THREADS)
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;\n" ::"r"(tma::smem_u32(to + at(i / PIECES, i % PIECES))), "l"(reinterpret_cast<const uint4*>(W) + i) : "memory");
+        asm volatile("cp.async.commit_group;\n" ::: "memory");
     }
-    __device__ __forceinline__ void pairs(int h, int i, uint32_t (&p)[4][1]) const { p[0][0] = w[h][i].x; p[1][0] = w[h][i].y; p[2][0] = w[h][i].z; p[3][0] = w[h][i].w; }
-};
-template <int D> struct MapRows<float, D> {
-    static constexpr int PARTS = 3;
-    float4 w[2][D / 16];
-    __device__ __forceinline__ void load(const float* W, int tig) {
+    // Channels 32 i + 8 tig .. + 7 of a row, as four pairs in PARTS bf16 parts.
+    __device__ __forceinline__ static void pairs(const unsigned char* from, int row, int i, int tig, uint32_t (&p)[4][PARTS]) {
+        if constexpr (PARTS == 1) {
+            const uint4 v = *reinterpret_cast<const uint4*>(from + at(row, 4 * i + tig));
+            p[0][0] = v.x; p[1][0] = v.y; p[2][0] = v.z; p[3][0] = v.w;
+        } else {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < D / 16; ++i) w[h][i] = *reinterpret_cast<const float4*>(W + h * 8 * D + 32 * (i / 2) + 8 * tig + 4 * (i % 2));
-    }
-    __device__ __forceinline__ void pairs(int h, int i, uint32_t (&p)[4][3]) const {
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            const float4 v = w[h][2 * i + j];
-            split_bf16<3>(v.x, v.y, p[2 * j]);
-            split_bf16<3>(v.z, v.w, p[2 * j + 1]);
+            for (int j = 0; j < 2; ++j) {
+                const float4 v = *reinterpret_cast<const float4*>(from + at(row, 8 * i + 2 * tig + j));
+                split_bf16<3>(v.x, v.y, p[2 * j]);
+                split_bf16<3>(v.z, v.w, p[2 * j + 1]);
+            }
         }
     }
 };
 
-// The records of a unit into its outputs.
-template <typename T, int D, typename TO>
-__global__ void __launch_bounds__(MERGE_THREADS)
-decode_q4_merge(const unsigned char* ws, Cache c, int g, Costs cost, int most_workers, const T* W, TO* __restrict__ out) {
-    constexpr int NW = MERGE_THREADS / 32, ROWS_W = 16;
+// The records of `seqs` sequences' units of one (layer, KV head) into their outputs: the map is fetched once for all of them.
+// HP: pairs of heads.
+template <typename T, int D, int HP, int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == MERGE_MOST ? 1 : sizeof(T) == 2 ? 4 : 3)
+decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, const T* W, void* __restrict__ out, int out_bf16) {
+    constexpr int NW = THREADS / 32, GROUPS = THREADS / MERGE_THREADS, ROWS_W = 16, heads = 2 * HP;
+    // Four numbers of a tier's sums are a thread's, ROUNDS times at the most: rows `row` and `row` + 8 of O tile t, heads 2 hp and 2 hp + 1.
+    constexpr int quads = D / 16 * HP * 8, ROUNDS = (2 * quads + MERGE_THREADS - 1) / MERGE_THREADS;
+    using Map = MapTile<T, D>;
+    extern __shared__ __align__(16) unsigned char map[];
     __shared__ __align__(16) float val[8][D + 4], keys[8][D + 4];
-    __shared__ float ref[8], inv[8], fac[2][8][MERGE_CHUNK];
-    const int u = blockIdx.x, b = u / c.LH, lh = u - b * c.LH;
+    __shared__ float ref[8], sum[8], scale[8], fac[2][8][MERGE_CHUNK];
+    __shared__ float2 ml[MERGE_CHUNK][2][8];
+    const int lh = blockIdx.x % c.LH, b0 = blockIdx.x / c.LH * seqs;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
-    MapRows<T, D> map;                   // requested ahead of the wait: the streaming kernel does not write it
-    if (wid < D / ROWS_W) map.load(W + ((size_t)lh * D + ROWS_W * wid + gid) * D, tig);
+    const int group = threadIdx.x / MERGE_THREADS, t0 = threadIdx.x % MERGE_THREADS;
+    Map::template request<THREADS>(map, W + (size_t)lh * D * D);           // ahead of the wait: the streaming kernel does not write it
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
-    const int64_t* prefix = reinterpret_cast<const int64_t*>(ws);
-    const float* records = reinterpret_cast<const float*>(ws + prefix_bytes(c.batch));
-    const int heads = even_heads(g), tier = tier_floats(g, D), units = c.batch * c.LH;
-    const int64_t p0 = prefix[b], p1 = prefix[b + 1], X = prefix[c.batch];
-    const int nr = tiles_of(rows_of(c.ret_len, b, c.ret_width)), na = tiles_of(rows_of(c.apx_len, b, c.apx_width));
-    TO* o = out + (size_t)u * g * D;
-    if (p0 == p1) {                                                   // nothing to attend to
-        for (int e = threadIdx.x; e < g * D; e += MERGE_THREADS) store_out(o + e, 0.f);
-        return;
-    }
-    const int64_t unit_cost = (int64_t)cost.ret * nr + (int64_t)cost.apx * na, from = p0 + lh * unit_cost;
-    const Deal deal(X, most_workers, cost);
-    const int w0 = deal.owner(from);
-    int last = deal.owner(from + unit_cost - 1);
-    if (last > w0 && tile_from(deal.begin(last) - from, nr, cost) >= nr + na) --last;       // its range begins within the unit's last tile
-    const int pieces = last - w0 + 1;                                 // the unit's own record, then those of workers w0 + 1 ..
-    const float *own = records + (size_t)u * 2 * tier, *others = records + (size_t)(units + w0) * 2 * tier;
-    auto piece = [&](int i) { return i == 0 ? own : others + (size_t)i * 2 * tier; };
-    // Four numbers of a tier's sums are a thread's: rows `row` and `row` + 8 of O tile t, heads 2 hp and 2 hp + 1.
-    const int quads = D / 16 * (heads / 2) * 8;
-    auto put = [&](int which, int i, float4 a) {
-        const int row = i & 7, hp = (i >> 3) % (heads / 2), t = (i >> 3) / (heads / 2);
-        float (*to)[D + 4] = which ? keys : val;                      // channel pairs 2 t and 2 t + 1 of piece row / 2
-        const int c0 = q4::Row<D>::channel_of(row / 2 * (D / 4) + 4 * t + row % 2), c1 = q4::Row<D>::channel_of(row / 2 * (D / 4) + 4 * t + 2 + row % 2);
-        to[2 * hp][c0] = a.x; to[2 * hp + 1][c0] = a.y; to[2 * hp][c1] = a.z; to[2 * hp + 1][c1] = a.w;
+    const int units = c.batch * c.LH;
+    constexpr int tier = heads * (D + 2);
+    auto put_out = [&](size_t at, float x) {
+        if (out_bf16) reinterpret_cast<__nv_bfloat16*>(out)[at] = __float2bfloat16_rn(x);
+        else reinterpret_cast<float*>(out)[at] = x;
     };
-    auto add = [](float4& a, float f0, float f1, const float4& v) {
-        a.x = fmaf(f0, v.x, a.x); a.y = fmaf(f1, v.y, a.y); a.z = fmaf(f0, v.z, a.z); a.w = fmaf(f1, v.w, a.w);
-    };
-    if (pieces <= FEW_PIECES) {
-        // everything a thread needs is requested at once: the heads' references and sums of all records, and its numbers
-        for (int e = threadIdx.x; e < 2 * quads; e += MERGE_THREADS) {
-            const int which = e >= quads, i = e - which * quads, hp = (i >> 3) % (heads / 2);
-            float4 ml[FEW_PIECES][2], v[FEW_PIECES];
-#pragma unroll
-            for (int k = 0; k < FEW_PIECES; ++k) {
-                ml[k][0] = ml[k][1] = make_float4(-INFINITY, 0.f, -INFINITY, 0.f);
-                v[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-                if (k < pieces) {
-                    ml[k][0] = *reinterpret_cast<const float4*>(piece(k) + 4 * hp);
-                    ml[k][1] = *reinterpret_cast<const float4*>(piece(k) + tier + 4 * hp);
-                    v[k] = *reinterpret_cast<const float4*>(piece(k) + which * tier + 2 * heads + 4 * i);
-                }
-            }
-            float M0 = -INFINITY, M1 = -INFINITY;
-#pragma unroll
-            for (int k = 0; k < FEW_PIECES; ++k)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) { M0 = fmaxf(M0, ml[k][r].x); M1 = fmaxf(M1, ml[k][r].z); }
-            float L0 = 0.f, L1 = 0.f;
-            float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll
-            for (int k = 0; k < FEW_PIECES; ++k)
-#pragma unroll
-                for (int r = 0; r < 2; ++r) {
-                    if (ml[k][r].x == -INFINITY && ml[k][r].z == -INFINITY) continue;      // no such record, or an empty one: its numbers are not any
-                    const float f0 = exp2f(ml[k][r].x - M0), f1 = exp2f(ml[k][r].z - M1);
-                    L0 = fmaf(f0, ml[k][r].y, L0); L1 = fmaf(f1, ml[k][r].w, L1);
-                    if (r == which) add(a, f0, f1, v[k]);
-                }
-            put(which, i, a);
-            if (which == 0 && i < 8 * (heads / 2) && (i & 7) == 0) { inv[2 * hp] = L0 == 0.f ? 0.f : 1.f / L0; inv[2 * hp + 1] = L1 == 0.f ? 0.f : 1.f / L1; }
+    for (int b = b0; b < min(b0 + seqs, c.batch); ++b) {
+        const int u = b * c.LH + lh;
+        const int n_apx = rows_of(c.apx_len, b, c.apx_width), n_ret = rows_of(c.ret_len, b, c.ret_width);
+        const int2 ends = reinterpret_cast<const int2*>(ws)[u];
+        const float* records = reinterpret_cast<const float*>(ws + ends_bytes(units));
+        const size_t o = (size_t)u * g * D;
+        if (n_ret + n_apx == 0) {                                     // nothing to attend to, and no record
+            for (int e = threadIdx.x; e < g * D; e += THREADS) put_out(o + e, 0.f);
+            continue;
         }
-    } else {
-        // a warp a head: the largest reference, the sum of the weights
-        for (int h = wid; h < heads; h += NW) {
-            float M = -INFINITY;
-            for (int i = lane; i < 2 * pieces; i += 32) M = fmaxf(M, piece(i >> 1)[(i & 1) * tier + 2 * h]);
-            M = warp_max(M);
-            float sum = 0.f;
-            for (int i = lane; i < 2 * pieces; i += 32) {
-                const float2 ml = *reinterpret_cast<const float2*>(piece(i >> 1) + (i & 1) * tier + 2 * h);
-                if (!(ml.x == -INFINITY)) sum = fmaf(exp2f(ml.x - M), ml.y, sum);
-            }
-            sum = warp_sum(sum);
-            if (lane == 0) { ref[h] = M; inv[h] = sum == 0.f ? 0.f : 1.f / sum; }
-        }
-        float4 a[D / 64] = {};                                        // at most D / 64 rounds of numbers, with eight heads
+        const int pieces = ends.y - ends.x + 1;                       // the unit's own record, then those of the workers behind its first
+        const float *own = records + (size_t)u * 2 * tier, *others = records + (size_t)(units + ends.x) * 2 * tier;
+        auto piece = [&](int i) { return i == 0 ? own : others + (size_t)i * 2 * tier; };
+        float4 a[ROUNDS] = {};
         for (int k0 = 0; k0 < pieces; k0 += MERGE_CHUNK) {
             const int n = min(pieces - k0, MERGE_CHUNK);
-            __syncthreads();
-            for (int e = threadIdx.x; e < 2 * heads * n; e += MERGE_THREADS) {
-                const int k = e / (2 * heads), r = e - k * 2 * heads, h = r >> 1, which = r & 1;
-                const float m = piece(k0 + k)[which * tier + 2 * h];
-                fac[which][h][k] = m == -INFINITY ? 0.f : exp2f(m - ref[h]);
+            constexpr int UN = 4;                                     // numbers of so many records are requested at a time
+            float4 v[UN];
+            auto request = [&](int j, int k) {
+                const int e = t0 + j * MERGE_THREADS, which = e >= quads, i = e - which * quads;
+                if (e >= 2 * quads) return;
+#pragma unroll
+                for (int z = 0; z < UN; ++z)
+                    if (k + z * GROUPS < n) v[z] = *reinterpret_cast<const float4*>(piece(k0 + k + z * GROUPS) + which * tier + 2 * heads + 4 * i);
+            };
+            for (int e = threadIdx.x; e < 2 * heads * n; e += THREADS) {
+                const int k = e / (2 * heads), r = e - k * 2 * heads, which = r >= heads, h = r - which * heads;
+                ml[k][which][h] = *reinterpret_cast<const float2*>(piece(k0 + k) + which * tier + 2 * h);
             }
+            request(0, group);
             __syncthreads();
-#pragma unroll
-            for (int j = 0; j < D / 64; ++j) {
-                const int e = threadIdx.x + j * MERGE_THREADS;
-                if (e >= 2 * quads) break;
-                const int which = e >= quads, i = e - which * quads, hp = (i >> 3) % (heads / 2);
-                const float *f0 = fac[which][2 * hp], *f1 = fac[which][2 * hp + 1];
-                constexpr int UN = 8;
-                for (int k = 0; k < n; k += UN) {
-                    float4 v[UN];
-#pragma unroll
-                    for (int z = 0; z < UN; ++z) {
-                        v[z] = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (k + z < n && (f0[k + z] != 0.f || f1[k + z] != 0.f))
-                            v[z] = *reinterpret_cast<const float4*>(piece(k0 + k + z) + which * tier + 2 * heads + 4 * i);
-                    }
-#pragma unroll
-                    for (int z = 0; z < UN; ++z)
-                        if (k + z < n) add(a[j], f0[k + z], f1[k + z], v[z]);
+            // a warp a head: the largest reference so far, what the sums so far and every record take against it
+            for (int h = wid; h < heads; h += NW) {
+                const float before = k0 ? ref[h] : -INFINITY;
+                float M = before;
+                for (int i = lane; i < 2 * n; i += 32) M = fmaxf(M, ml[i >> 1][i & 1][h].x);
+                M = warp_max(M);
+                float L = 0.f;
+                for (int i = lane; i < 2 * n; i += 32) {
+                    const float2 x = ml[i >> 1][i & 1][h];
+                    const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);      // an empty record's sum and numbers are not any
+                    if (f != 0.f) L = fmaf(f, x.y, L);
+                    fac[i & 1][h][i >> 1] = f;
+                }
+                L = warp_sum(L);
+                if (lane == 0) {
+                    const float f = before == -INFINITY ? 0.f : exp2f(before - M);
+                    scale[h] = f;
+                    ref[h] = M;
+                    sum[h] = k0 ? fmaf(f, sum[h], L) : L;
                 }
             }
+            __syncthreads();
+#pragma unroll
+            for (int j = 0; j < ROUNDS; ++j) {
+                const int e = t0 + j * MERGE_THREADS, which = e >= quads, i = e - which * quads, hp = (i >> 3) % HP;
+                if (e >= 2 * quads) break;
+                const float *f0 = fac[which][2 * hp], *f1 = fac[which][2 * hp + 1];
+                if (k0) { const float s0 = scale[2 * hp], s1 = scale[2 * hp + 1]; a[j].x *= s0; a[j].y *= s1; a[j].z *= s0; a[j].w *= s1; }
+                if (j) request(j, group);
+                for (int k = group; k < n;) {
+                    const float4 w[UN] = {v[0], v[1], v[2], v[3]};
+                    const int at = k;
+                    if ((k += UN * GROUPS) < n) request(j, k);
+#pragma unroll
+                    for (int z = 0; z < UN; ++z) {
+                        if (at + z * GROUPS >= n) break;
+                        const float x0 = f0[at + z * GROUPS], x1 = f1[at + z * GROUPS];
+                        if (x0 == 0.f && x1 == 0.f) continue;
+                        a[j].x = fmaf(x0, w[z].x, a[j].x); a[j].y = fmaf(x1, w[z].y, a[j].y); a[j].z = fmaf(x0, w[z].z, a[j].z); a[j].w = fmaf(x1, w[z].w, a[j].w);
+                    }
+                }
+            }
+            if (k0 + MERGE_CHUNK < pieces) __syncthreads();
         }
+        // the groups' sums, one after another
 #pragma unroll
-        for (int j = 0; j < D / 64; ++j) {
-            const int e = threadIdx.x + j * MERGE_THREADS;
-            if (e < 2 * quads) put(e >= quads, e >= quads ? e - quads : e, a[j]);
+        for (int q = 0; q < GROUPS; ++q) {
+            if (group == q) {
+#pragma unroll
+                for (int j = 0; j < ROUNDS; ++j) {
+                    const int e = t0 + j * MERGE_THREADS, which = e >= quads, i = e - which * quads;
+                    if (e >= 2 * quads) break;
+                    const int row = i & 7, hp = (i >> 3) % HP, t = (i >> 3) / HP;
+                    float (*to)[D + 4] = which ? keys : val;          // channel pairs 2 t and 2 t + 1 of piece row / 2
+                    const int c0 = q4::Row<D>::channel_of(row / 2 * (D / 4) + 4 * t + row % 2), c1 = q4::Row<D>::channel_of(row / 2 * (D / 4) + 4 * t + 2 + row % 2);
+                    if (q) { a[j].x += to[2 * hp][c0]; a[j].y += to[2 * hp + 1][c0]; a[j].z += to[2 * hp][c1]; a[j].w += to[2 * hp + 1][c1]; }
+                    to[2 * hp][c0] = a[j].x; to[2 * hp + 1][c0] = a[j].y; to[2 * hp][c1] = a[j].z; to[2 * hp + 1][c1] = a[j].w;
+                }
+            }
+            if (q + 1 < GROUPS) __syncthreads();
         }
-    }
-    __syncthreads();
-    // ---- the map: its rows down, heads across; the key sums, and an fp32 map, in three bf16 parts, products down to 2^-16 of the largest
-    if (wid >= D / ROWS_W) return;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    if (na > 0) {
-        const int head = min(gid, heads - 1);
+        asm volatile("cp.async.wait_group 0;\n" ::: "memory");
+        __syncthreads();
+        // ---- the map: its rows down, heads across; the key sums, and an fp32 map, in three bf16 parts, products down to 2^-16 of the largest
+        if (wid < D / ROWS_W) {
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+            if (n_apx > 0) {
+                const int head = min(gid, heads - 1);
 #pragma unroll
-        for (int i = 0; i < D / 32; ++i) {
-            constexpr int P = MapRows<T, D>::PARTS;
-            uint32_t r0[4][P], r1[4][P], part[4][3];
-            map.pairs(0, i, r0);
-            map.pairs(1, i, r1);
-            const float4 k0 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig]), k1 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig + 4]);
-            split_bf16<3>(k0.x, k0.y, part[0]); split_bf16<3>(k0.z, k0.w, part[1]);
-            split_bf16<3>(k1.x, k1.y, part[2]); split_bf16<3>(k1.z, k1.w, part[3]);
+                for (int i = 0; i < D / 32; ++i) {
+                    constexpr int P = Map::PARTS;
+                    uint32_t r0[4][P], r1[4][P], part[4][3];
+                    Map::pairs(map, ROWS_W * wid + gid, i, tig, r0);
+                    Map::pairs(map, ROWS_W * wid + 8 + gid, i, tig, r1);
+                    const float4 x0 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig]), x1 = *reinterpret_cast<const float4*>(&keys[head][32 * i + 8 * tig + 4]);
+                    split_bf16<3>(x0.x, x0.y, part[0]); split_bf16<3>(x0.z, x0.w, part[1]);
+                    split_bf16<3>(x1.x, x1.y, part[2]); split_bf16<3>(x1.z, x1.w, part[3]);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int s = 0; s < 2; ++s) {
+                        float once[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int p = 2; p >= 0; --p)
+                        for (int p = 2; p >= 0; --p)
 #pragma unroll
-                    for (int r = P - 1; r >= 0; --r)
-                        if (p + r <= 2)
-                            asm volatile(
-                                "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
-                                : "+f"(sum[0]), "+f"(sum[1]), "+f"(sum[2]), "+f"(sum[3])
-                                : "r"(r0[2 * s][r]), "r"(r1[2 * s][r]), "r"(r0[2 * s + 1][r]), "r"(r1[2 * s + 1][r]), "r"(part[2 * s][p]), "r"(part[2 * s + 1][p]));
+                            for (int r = P - 1; r >= 0; --r)
+                                if (p + r <= 2)
+                                    asm volatile(
+                                        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
+                                        : "+f"(once[0]), "+f"(once[1]), "+f"(once[2]), "+f"(once[3])
+                                        : "r"(r0[2 * s][r]), "r"(r1[2 * s][r]), "r"(r0[2 * s + 1][r]), "r"(r1[2 * s + 1][r]), "r"(part[2 * s][p]), "r"(part[2 * s + 1][p]));
 #pragma unroll
-                for (int e = 0; e < 4; ++e) acc[e] += sum[e];
+                        for (int e = 0; e < 4; ++e) acc[e] += once[e];
+                    }
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int h = 2 * tig + (e & 1), ch = ROWS_W * wid + 8 * (e >> 1) + gid;
+                if (h < g) put_out(o + h * D + ch, sum[h] == 0.f ? 0.f : (val[h][ch] + acc[e]) / sum[h]);
             }
         }
+        __syncthreads();                                              // the sums are free for the next sequence
     }
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const int h = 2 * tig + (e & 1), ch = ROWS_W * wid + 8 * (e >> 1) + gid;
-        if (h < g) store_out(o + h * D + ch, (val[h][ch] + acc[e]) * inv[h]);
-    }
+    asm volatile("cp.async.wait_group 0;\n" ::: "memory");
 }
 
 }  // namespace dq4
