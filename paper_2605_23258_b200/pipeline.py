@@ -97,3 +97,66 @@ class Compressor:
     def decode(self, q, W, out, mode: int = 0):
         B.vector_decode_attn(self.shape, q, self.cache, W, out, mode, self.ws)
         return out
+
+
+class PagedCache:
+    """The compressed caches of many requests in 4 bits and pages, one place of a batch each: requests are admitted with a compressed context,
+    grow by a generated token a step, and end, each with a length of its own.
+
+    shape.batch is the number of places; all device work is asynchronous on the current stream, and `append` and `decode` read nothing back, so
+    that a captured step follows the requests' lengths. 
+    """
+
+    def __init__(self, shape: B.Shape, ret_pages: int, apx_pages: int, ret_rows: int, apx_rows: int, positions: bool = True, device="cuda"):
+        """Pools of so many pages; places for at most ret_rows retained and apx_rows key-only rows of a request."""
+        self.shape, self.device = shape, device
+        pages = lambda rows: max(-(-rows // B.VECTOR_PAGE_ROWS), 1)  # noqa: E731
+        self.cache = B.alloc_q4_cache(shape, ret_pages, apx_pages, pages(ret_rows), pages(apx_rows), positions, device)
+        n = shape.batch
+        ints = lambda *size: torch.zeros(*size, dtype=torch.int32, device=device)  # noqa: E731
+        # stacks of free pages, the first page on top
+        self.ret_free, self.apx_free = (torch.arange(p - 1, -1, -1, dtype=torch.int32, device=device) for p in (ret_pages, apx_pages))
+        self.n_ret_free, self.n_apx_free = ints(1).fill_(ret_pages), ints(1).fill_(apx_pages)
+        self.active, self.first_row, self.row_start, self.slots = ints(n), ints(n), ints(n + 1), ints(n)
+        self.ws = torch.empty(B.vector_decode_q4_workspace_bytes(shape), dtype=torch.uint8, device=device)
+
+    def _change(self, tier: str, added, slots=None):
+        c = self.cache
+        table, length, stack, left = ((c.ret_table, c.ret_len, self.ret_free, self.n_ret_free) if tier == "ret"
+                                      else (c.apx_table, c.apx_len, self.apx_free, self.n_apx_free))
+        B.vector_block_tables(length, added, B.VECTOR_PAGE_ROWS, table, stack, left, length, left, self.first_row, self.row_start, slots)
+
+    def admit(self, place: int, comp: Compressor, K, V):
+        """Takes the routed context of a Compressor of one sequence (its score and route have been called) to an empty place."""
+        sh, b = comp.shape, comp.budget
+        if sh.batch != 1 or (sh.n_layers, sh.n_kv_heads, sh.head_dim, sh.dtype) != (self.shape.n_layers, self.shape.n_kv_heads, self.shape.head_dim, self.shape.dtype):
+            raise ValueError("the compressor is for one sequence of the same layers and heads")
+        slots = {}
+        for tier, n in (("ret", b.n_ret), ("apx", b.n_apx)):
+            slots[tier] = torch.empty(n, dtype=torch.int32, device=self.device)
+            added = torch.zeros(self.shape.batch, dtype=torch.int32, device=self.device)
+            added[place] = n
+            self._change(tier, added, slots[tier])
+        B.vector_compact_q4(sh, b, K, V, comp.ret_idx, comp.apx_idx, self.cache, slots["ret"], slots["apx"])
+        self.active[place] = 1
+
+    def end(self, *places: int):
+        """Gives the pages of these places back."""
+        gone = torch.zeros(self.shape.batch, dtype=torch.int32, device=self.device)
+        gone[list(places)] = -2**31
+        for tier in ("ret", "apx"):
+            self._change(tier, gone)
+        self.active[list(places)] = 0
+
+    def append(self, k_new, v_new, pos):
+        """A generated token of every active place: k_new, v_new [U][d], pos [batch] int32.  A request that finds no page left keeps its length."""
+        self._change("ret", self.active, self.slots)
+        B.vector_append_q4(self.shape, self.cache, k_new, v_new, self.row_start, self.slots, pos)
+
+    def decode(self, q, W, out):
+        B.vector_decode_attn_q4(self.shape, q, self.cache, W, out, self.ws)
+        return out
+
+    def free_pages(self) -> tuple[int, int]:
+        """Pages left in the two pools (waits for the device)."""
+        return int(self.n_ret_free), int(self.n_apx_free)
