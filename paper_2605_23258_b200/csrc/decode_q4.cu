@@ -14,10 +14,10 @@ static size_t ws_bytes_of(const Dims& dm) {
 struct Call {
     const Dims& dm; const void* q; Cache c; const void* W; void* out; int out_dtype; unsigned char* ws; cudaStream_t st;
 
-    template <typename T, int D, bool ROPE, bool EXACT> vector_status both() const {
-        using C = Cfg<T, D, ROPE, EXACT>;
+    template <typename T, int D, bool ROPE, bool EXACT, bool FOLD> vector_status both() const {
+        using C = Cfg<T, D, ROPE, EXACT, FOLD>;
         static_assert(C::WARPS <= MOST_WARPS && C::SMEM_BYTES + (MAX_BATCH + 1) * 8 + 2048 <= 227 * 1024, "a block's shared memory, its own variables included");
-        auto kern = decode_q4_stream<T, D, ROPE, EXACT>;
+        auto kern = decode_q4_stream<T, D, ROPE, EXACT, FOLD>;
         static PerDeviceOnce once;
         if (once.first()) {
             const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM_BYTES + (MAX_BATCH + 1) * 8);
@@ -27,7 +27,7 @@ struct Call {
         if (!fault) return VECTOR_ERR_CUDA;
         RopePhases ph = {};
         if (ROPE) rope_phases(dm.theta, D, &ph);
-        VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::SMEM_BYTES + (size_t)(c.batch + 1) * 8, st, (const T*)q, c, dm.g, C::COST,
+        VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::SMEM_BYTES + (size_t)(c.batch + 1) * 8, st, (const T*)q, c, dm.g,
                                               dm.scale * 1.4426950408889634f, ws, fault, ph));
         return merge<T, D>();
     }
@@ -59,8 +59,9 @@ struct Call {
     template <typename T, int D> vector_status run() const {
         const bool exact = dm.dtype == VECTOR_F32 || out_dtype == VECTOR_F32;
         if constexpr (sizeof(T) == 2)
-            if (!exact) return dm.rope ? both<T, D, true, false>() : both<T, D, false, false>();
-        return dm.rope ? both<T, D, true, true>() : both<T, D, false, true>();
+            if (!exact) return dm.rope ? both<T, D, true, false, false>() : both<T, D, false, false, false>();
+        if (dm.g <= 4) return dm.rope ? both<T, D, true, true, true>() : both<T, D, false, true, true>();
+        return dm.rope ? both<T, D, true, true, false>() : both<T, D, false, true, false>();
     }
 };
 

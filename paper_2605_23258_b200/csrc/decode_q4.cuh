@@ -35,10 +35,7 @@ namespace dq4 {
 
 constexpr int MAX_BATCH = VECTOR_Q4_MAX_BATCH;
 // What a tile of either tier costs a worker, in small numbers.
-struct Costs {
-    int ret, apx;
-    __host__ __device__ int most() const { return ret > apx ? ret : apx; }
-};
+template <int RET, int APX> struct Costs { static constexpr int ret = RET, apx = APX, most = RET > APX ? RET : APX; };
 constexpr float SLACK = 8.f;
 
 struct Cache {
@@ -57,22 +54,35 @@ __host__ __device__ inline size_t ends_bytes(int units) { return ((size_t)units 
 __host__ __device__ inline int even_heads(int g) { return (g + 1) & ~1; }
 __host__ __device__ inline int tier_floats(int g, int d) { return even_heads(g) * (d + 2); }
 
-// How the cost X of all tiles is dealt to workers.  Every range is as long as a tile's cost at the least, so each begins a tile.
+// How the cost X of all tiles is dealt to workers.  Every range is as long as a tile at the least, so each begins one.  Where there is work for all workers the
+// bounds are the multiples of one fp64 number, the same for all who ask, and a range of more than a tile; where there is not, whole numbers.
 struct Deal {
     int64_t X;
     int workers;
-    __device__ __forceinline__ Deal(int64_t x, int workers_at_most, Costs cost)
-        : X(x), workers((int)max(min((int64_t)workers_at_most, x / cost.most()), (int64_t)1)) {}
-    __device__ __forceinline__ int64_t begin(int w) const { return X * w / workers; }
+    double step;                    // 0: few tiles
+    __device__ __forceinline__ Deal(int64_t x, int workers_at_most, int most_cost) : X(x), workers(workers_at_most), step(0.) {
+        if (x > (int64_t)workers_at_most * (most_cost + 1)) step = (double)x / workers_at_most;
+        else workers = max(min((int)x / most_cost, workers_at_most), 1);
+    }
+    __device__ __forceinline__ int64_t begin(int w) const {
+        if (w == workers) return X;
+        return step > 0. ? (int64_t)(step * w) : (int64_t)((uint32_t)X * (uint32_t)w / (uint32_t)workers);      // under 2^32: X is a few times the workers there
+    }
 };
+// a / b, in 32 bits where they do.
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b) {
+    return ((a | b) >> 32) == 0 ? (int64_t)((uint32_t)a / (uint32_t)b) : a / b;
+}
 // First tile of a unit that begins at r or later, r counted from the unit's beginning.
-__device__ __forceinline__ int tile_from(int64_t r, int nr, Costs cost) {
-    const int64_t ret = (int64_t)cost.ret * nr;
-    return r <= ret ? (int)((r + cost.ret - 1) / cost.ret) : nr + (int)((r - ret + cost.apx - 1) / cost.apx);
+template <typename Cost> __device__ __forceinline__ int tile_from(int64_t r, int nr) {
+    const int64_t ret = (int64_t)Cost::ret * nr;
+    return r <= ret ? (int)((r + Cost::ret - 1) / Cost::ret) : nr + (int)((r - ret + Cost::apx - 1) / Cost::apx);
 }
 
-template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
-    static constexpr int WARPS = EXACT && D == 128 ? 8 : 12;
+// FOLD: EXACT with at most four heads, whose first and second parts of weights are eight columns of one product.
+template <typename T, int D, bool ROPE, bool EXACT, bool FOLD> struct Cfg {
+    static_assert(EXACT || !FOLD, "one part needs no folding");
+    static constexpr int WARPS = EXACT && D == 128 && (!FOLD || ROPE || sizeof(T) == 4) ? 8 : 12;
     static constexpr int ENTRIES = WARPS == 12 ? 3 : 4;                // of a warp's ring, a tile each
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int POS_AT = q4::Row<D>::TILE;                    // of a key-only tile's positions, within an entry
@@ -82,7 +92,7 @@ template <typename T, int D, bool ROPE, bool EXACT> struct Cfg {
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
     static constexpr int N_APX = ROPE ? 1 : 2;                         // key-only rows of a step, in sixteens
-    static constexpr Costs COST = ROPE ? Costs{2, 3} : Costs{4, 3};
+    using Cost = std::conditional_t<ROPE, Costs<2, 3>, Costs<4, 3>>;
 };
 
 // Not volatile, like the transposes: the compiler may move them past one another, so that one's operands are on their way during the next.
@@ -120,8 +130,7 @@ __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
 // A worker's way through the sequence of tiles, as runs: tiles of one tier of one unit.
-struct Runs {
-    Costs cost;
+template <typename Cost> struct Runs {
     int64_t left;                               // cost up to the end of the worker's range
     int b, lh, n_ret, n_apx;                    // sequence, (layer, KV head), rows
     int apx, p, count;                          // the run: tier, first tile of it, tiles
@@ -142,8 +151,8 @@ struct Runs {
         }
         apx = t >= nr;
         p = apx ? t - nr : t;
-        const int each = apx ? cost.apx : cost.ret;
-        const int64_t in_range = (left + each - 1) / each;
+        const int each = apx ? Cost::apx : Cost::ret;
+        const int64_t in_range = apx ? (left + Cost::apx - 1) / Cost::apx : (left + Cost::ret - 1) / Cost::ret;
         count = b < c.batch ? (int)max(min((int64_t)((apx ? tiles_of(n_apx) : nr) - p), in_range), (int64_t)0) : 0;
         left -= (int64_t)count * each;
     }
@@ -158,11 +167,12 @@ struct Runs {
         }
         b = lo;
         enter(c);
-        const int64_t unit = (prefix[b + 1] - prefix[b]) / c.LH;
-        lh = (int)((x - prefix[b]) / unit);
+        const int nr = tiles_of(n_ret);
+        const int64_t unit = (int64_t)Cost::ret * nr + (int64_t)Cost::apx * tiles_of(n_apx);
+        lh = (int)divide(x - prefix[b], unit);
         const int64_t r = x - prefix[b] - lh * unit;
-        const int nr = tiles_of(n_ret), t = tile_from(r, nr, cost);
-        left = end - x - ((int64_t)cost.ret * min(t, nr) + (int64_t)cost.apx * max(t - nr, 0) - r);
+        const int t = tile_from<Cost>(r, nr);
+        left = end - x - ((int64_t)Cost::ret * min(t, nr) + (int64_t)Cost::apx * max(t - nr, 0) - r);
         run(c, prefix, t);
     }
 };
@@ -195,10 +205,10 @@ template <int N> __device__ __forceinline__ void load_run(const __nv_bfloat16* p
     }
 }
 
-template <typename T, int D, bool ROPE, bool EXACT>
-__global__ void __launch_bounds__(Cfg<T, D, ROPE, EXACT>::THREADS, 1)
-decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsigned char* ws, int* fault, RopePhases phases) {
-    using C = Cfg<T, D, ROPE, EXACT>;
+template <typename T, int D, bool ROPE, bool EXACT, bool FOLD>
+__global__ void __launch_bounds__(Cfg<T, D, ROPE, EXACT, FOLD>::THREADS, 1)
+decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* ws, int* fault, RopePhases phases) {
+    using C = Cfg<T, D, ROPE, EXACT, FOLD>;
     using R = q4::Row<D>;
     constexpr int WARPS = C::WARPS, ENTRIES = C::ENTRIES;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -228,7 +238,7 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
         const int b = b0 + threadIdx.x;
         int64_t x = 0;
         if (b < c.batch)
-            x = (int64_t)c.LH * ((int64_t)cost.ret * tiles_of(rows_of(c.ret_len, b, c.ret_width)) + (int64_t)cost.apx * tiles_of(rows_of(c.apx_len, b, c.apx_width)));
+            x = (int64_t)c.LH * ((int64_t)C::Cost::ret * tiles_of(rows_of(c.ret_len, b, c.ret_width)) + (int64_t)C::Cost::apx * tiles_of(rows_of(c.apx_len, b, c.apx_width)));
         int64_t s = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -246,7 +256,7 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
     }
     if (threadIdx.x == 0) prefix[c.batch] = carry;
     __syncthreads();
-    const Deal deal(carry, gridDim.x * WARPS, cost);
+    const Deal deal(carry, gridDim.x * WARPS, C::Cost::most);
     const int worker = wid * gridDim.x + blockIdx.x;        // neighbours in the sequence on different multiprocessors
     if (carry == 0 || worker >= deal.workers) return;
 
@@ -257,8 +267,7 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
     const uint64_t policy = tma::policy_evict_first();
 
     // ---- the producing side, ENTRIES ahead: `run` is where it is, `k` tiles of it are on their way, and lane l has the page of tile l of 32
-    Runs run;
-    run.cost = cost;
+    Runs<typename C::Cost> run;
     run.find(c, prefix, deal.begin(worker), deal.begin(worker + 1));
     int k = 0, page = -1, values = 0;
     auto issue = [&](int s) {
@@ -306,11 +315,12 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
     clear();
     // The queries of a unit as B fragments: head gid, the channels of piece tig.  Scaled so that the largest lies in [2^7, 2^8).
     auto load_queries = [&](int unit) {
-        const T* row = q + ((size_t)unit * g + min(gid, g - 1)) * D + tig * (D / 8);
+        const int head = FOLD ? gid & 3 : gid;
+        const T* row = q + ((size_t)unit * g + min(head, g - 1)) * D + tig * (D / 8);
         float x[2 * C::PAIRS];
 #pragma unroll
         for (int h = 0; h < 2; ++h) load_run<C::PAIRS>(row + h * (D / 2), &x[h * C::PAIRS]);
-        if (gid >= g) {
+        if (head >= g) {
 #pragma unroll
             for (int i = 0; i < 2 * C::PAIRS; ++i) x[i] = 0.f;
         }
@@ -410,10 +420,13 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
             for (int h = 0; h < 2; ++h) {
                 const float a = tc::ex2(fmaf(S[i][2 * h], fac[0], -m[0])), b = tc::ex2(fmaf(S[i][2 * h + 1], fac[1], -m[1]));
                 const uint32_t hi = pack_h2(a, b);
-                ph[i][h] = transpose(hi);
                 if constexpr (EXACT) {
                     const float2 f = unpack_h2(hi);
-                    pl[i][h] = transpose(pack_h2(a - f.x, b - f.y));
+                    const uint32_t low = pack_h2(a - f.x, b - f.y);
+                    ph[i][h] = transpose(FOLD && tig >= 2 ? low : hi);
+                    if constexpr (!FOLD) pl[i][h] = transpose(low);
+                } else {
+                    ph[i][h] = transpose(hi);
                 }
             }
     };
@@ -424,7 +437,7 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
             const uint32_t a0 = transpose(x[0][2 * t]), a1 = transpose(x[0][2 * t + 1]), a2 = transpose(x[1][2 * t]), a3 = transpose(x[1][2 * t + 1]);
             if constexpr (EXACT) {
                 float sum[4] = {0.f, 0.f, 0.f, 0.f};
-                mma(sum, a0, a1, a2, a3, pl[0], pl[1]);
+                if constexpr (!FOLD) mma(sum, a0, a1, a2, a3, pl[0], pl[1]);
                 if constexpr (with_lo.value) mma(sum, transpose(lo[0][2 * t]), transpose(lo[0][2 * t + 1]), transpose(lo[1][2 * t]), transpose(lo[1][2 * t + 1]), ph[0], ph[1]);
                 mma(sum, a0, a1, a2, a3, ph[0], ph[1]);
 #pragma unroll
@@ -435,7 +448,7 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
         }
         constexpr uint32_t ONE = 0x3c003c00u;
         float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (EXACT) mma(sum, ONE, ONE, ONE, ONE, pl[0], pl[1]);
+        if constexpr (EXACT && !FOLD) mma(sum, ONE, ONE, ONE, ONE, pl[0], pl[1]);
         mma(sum, ONE, ONE, ONE, ONE, ph[0], ph[1]);
         L[0] += sum[0]; L[1] += sum[1];
     };
@@ -482,6 +495,15 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
     // The state of a tier to its record; an empty one's sums are not read.
     auto put_tier = [&](int tier, bool empty) {
         float* p = records + (size_t)slot_rec * rec + tier * tier_floats(g, D);
+        if constexpr (FOLD)
+            if (!empty) {                                              // columns of first and second parts become one
+#pragma unroll
+                for (int t = 0; t < C::O_TILES; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) O[t][e] += __shfl_xor_sync(0xffffffffu, O[t][e], 2);
+#pragma unroll
+                for (int h = 0; h < 2; ++h) L[h] += __shfl_xor_sync(0xffffffffu, L[h], 2);
+            }
         if (2 * tig >= heads) return;
         if (gid == 0) *reinterpret_cast<float4*>(p + 4 * tig) = empty ? make_float4(-INFINITY, 0.f, -INFINITY, 0.f) : make_float4(m[0], L[0], m[1], L[1]);
         if (empty) return;
@@ -517,6 +539,8 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
         __syncwarp();
     };
+    bool fresh = false;                                                // whether a unit's queries are still to be fetched
+    if (ahead > 0) load_queries(entries[wid][0].unit);                 // while the first tile is on its way
     while (ahead > 0) {
         if (!wait()) return;
         const Entry entry = entries[wid][at];
@@ -526,7 +550,8 @@ decode_q4_stream(const T* q, Cache c, int g, Costs cost, float scale_log2e, unsi
             unit = entry.unit; apx = tier; wrote = 0;
             slot_rec = entry.edge & 1 ? unit : units + worker;
             clear();
-            load_queries(unit);
+            if (fresh) load_queries(unit);
+            fresh = true;
         } else if (tier != apx) {
             put_tier(apx, false);
             wrote |= 1 << apx;
