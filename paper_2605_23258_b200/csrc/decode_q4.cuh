@@ -91,7 +91,9 @@ template <typename T, int D, bool ROPE, bool EXACT, bool FOLD> struct Cfg {
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
-    static constexpr int N_APX = ROPE ? 1 : 2;                         // key-only rows of a step, in sixteens
+    // Rows of a softmax step, in sixteens.  us by (retained, key-only): 640 units of 3300 and 6550 rows (2, 1) 181, (1, 1) 181, (2, 2) 187; 2048 units of 650 and 1120 rows
+    // 124, 125, 134; rotary keys, 128 units of 3000 and 6000 rows 65.6, 66.8, 71.9; 64 channels, fp32 results 44.0, 44.8, 42.1.
+    static constexpr int N_RET = 2, N_APX = D == 64 && !ROPE ? 2 : 1;
     using Cost = std::conditional_t<ROPE, Costs<2, 3>, Costs<4, 3>>;
 };
 
@@ -101,6 +103,12 @@ __device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uin
         "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};\n"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// The same product on its own: nothing to add it to, and no registers to clear for that.
+__device__ __forceinline__ void mma_alone(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t transpose(uint32_t a) {
     uint32_t r;
@@ -305,12 +313,12 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
 
     // ---- the consuming side
     uint32_t qb[C::Q_PARTS][C::O_TILES][2];
-    float fac[2] = {0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, O[C::O_TILES][4], L[2];
+    float fac[2] = {0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, O[C::O_TILES][4], L[4];
     auto clear = [&] {
         m[0] = m[1] = -INFINITY;
 #pragma unroll
         for (int t = 0; t < C::O_TILES; ++t) O[t][0] = O[t][1] = O[t][2] = O[t][3] = 0.f;
-        L[0] = L[1] = 0.f;
+        L[0] = L[1] = L[2] = L[3] = 0.f;                               // L: the same sums in all rows, of which two numbers are used
     };
     clear();
     // The queries of a unit as B fragments: head gid, the channels of piece tig.  Scaled so that the largest lies in [2^7, 2^8).
@@ -358,8 +366,8 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 const uint2 v = *reinterpret_cast<const uint2*>(tile + row * R::CODES + tig * 8);
                 w[0] = v.x; w[1] = v.y;
             }
-            const uint32_t s = *reinterpret_cast<const uint16_t*>(tile + R::SCALES_AT + row * R::GROUPS + 2 * (D == 128 ? tig : tig >> 1));
-            const uint32_t s2[2] = {(s & 0xffu) * 0x00800080u, (s >> 8) * 0x00800080u};
+            const unsigned char* s = tile + R::SCALES_AT + row * R::GROUPS + 2 * (D == 128 ? tig : tig >> 1);
+            const uint32_t s2[2] = {s[0] * 0x00800080u, s[1] * 0x00800080u};
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 uint32_t p[4];
@@ -371,17 +379,20 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     };
     // Logits of 16 keys, in chains of two products (EXACT) or of half of them.
     auto logits = [&](const uint32_t (&x)[2][C::PAIRS], float (&S)[4]) {
-        S[0] = S[1] = S[2] = S[3] = 0.f;
         constexpr int CHAIN = EXACT ? 2 : C::O_TILES / 2;
 #pragma unroll
         for (int p = C::Q_PARTS - 1; p >= 0; --p)
 #pragma unroll
             for (int t0 = 0; t0 < C::O_TILES; t0 += CHAIN) {
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                float sum[4];
 #pragma unroll
-                for (int t = t0; t < t0 + CHAIN; ++t) mma(sum, x[0][2 * t], x[1][2 * t], x[0][2 * t + 1], x[1][2 * t + 1], qb[p][t][0], qb[p][t][1]);
+                for (int t = t0; t < t0 + CHAIN; ++t) {
+                    const uint32_t a0 = x[0][2 * t], a1 = x[1][2 * t], a2 = x[0][2 * t + 1], a3 = x[1][2 * t + 1];
+                    if (t == t0) mma_alone(sum, a0, a1, a2, a3, qb[p][t][0], qb[p][t][1]);
+                    else mma(sum, a0, a1, a2, a3, qb[p][t][0], qb[p][t][1]);
+                }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[e] += sum[e];
+                for (int e = 0; e < 4; ++e) S[e] = p == C::Q_PARTS - 1 && t0 == 0 ? sum[e] : S[e] + sum[e];
             }
     };
     // Weights of N x 16 keys, of which `rows` are there, from their logits, against the reference m (fac > 0); as B fragments.
@@ -411,7 +422,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 m[h] = now;
 #pragma unroll
                 for (int t = 0; t < C::O_TILES; ++t) { O[t][h] *= f; O[t][2 + h] *= f; }
-                L[h] *= f;
+                L[h] *= f; L[2 + h] *= f;
             }
         }
 #pragma unroll
@@ -436,10 +447,10 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         for (int t = 0; t < C::O_TILES; ++t) {
             const uint32_t a0 = transpose(x[0][2 * t]), a1 = transpose(x[0][2 * t + 1]), a2 = transpose(x[1][2 * t]), a3 = transpose(x[1][2 * t + 1]);
             if constexpr (EXACT) {
-                float sum[4] = {0.f, 0.f, 0.f, 0.f};
+                float sum[4];
+                mma_alone(sum, a0, a1, a2, a3, ph[0], ph[1]);
                 if constexpr (!FOLD) mma(sum, a0, a1, a2, a3, pl[0], pl[1]);
                 if constexpr (with_lo.value) mma(sum, transpose(lo[0][2 * t]), transpose(lo[0][2 * t + 1]), transpose(lo[1][2 * t]), transpose(lo[1][2 * t + 1]), ph[0], ph[1]);
-                mma(sum, a0, a1, a2, a3, ph[0], ph[1]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[t][e] += sum[e];
             } else {
@@ -447,10 +458,14 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             }
         }
         constexpr uint32_t ONE = 0x3c003c00u;
-        float sum[4] = {0.f, 0.f, 0.f, 0.f};
-        if constexpr (EXACT && !FOLD) mma(sum, ONE, ONE, ONE, ONE, pl[0], pl[1]);
-        mma(sum, ONE, ONE, ONE, ONE, ph[0], ph[1]);
-        L[0] += sum[0]; L[1] += sum[1];
+        if constexpr (EXACT) {
+            float sum[4];
+            mma_alone(sum, ONE, ONE, ONE, ONE, ph[0], ph[1]);
+            if constexpr (!FOLD) mma(sum, ONE, ONE, ONE, ONE, pl[0], pl[1]);
+            L[0] += sum[0]; L[1] += sum[1];
+        } else {
+            mma(L, ONE, ONE, ONE, ONE, ph[0], ph[1]);
+        }
     };
 
     // The 16 rows at row0 turned back by their positions; lo: second parts.
@@ -569,19 +584,20 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             if (++at == ENTRIES) { at = 0; phase ^= 1; }
             if (!wait()) return;
             tile = ring + at * C::ENTRY_BYTES;
+            constexpr int N = C::N_RET;
             if (entry.rows < q4::ROWS) blank(tile, entry.rows);
 #pragma unroll 1
-            for (int row0 = 0; row0 < entry.rows; row0 += 32) {
-                uint32_t x[2][C::PAIRS], ph[2][2], pl[2][2];
-                float S[2][4];
+            for (int row0 = 0; row0 < entry.rows; row0 += 16 * N) {
+                uint32_t x[2][C::PAIRS], ph[N][2], pl[N][2];
+                float S[N][4];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < N; ++i) {
                     load_rows(keys, row0 + 16 * i, x);
                     logits(x, S[i]);
                 }
                 weigh(S, entry.rows - row0, ph, pl);
 #pragma unroll
-                for (int i = 0; i < 2; ++i) {
+                for (int i = 0; i < N; ++i) {
                     load_rows(tile, row0 + 16 * i, x);
                     add_rows(x, ph[i], pl[i], x, std::false_type());
                 }
