@@ -382,8 +382,8 @@ VECTOR_API size_t vector_q4_tile_bytes(const vector_shape* shape);
  * is all added rows; slots[row_start[b] + i]: the slot of its i-th added row, -1 where it got no page for it; slots behind the last added row are -1.  new_n_free:
  * the pages that are left on the stack.  new_lengths may be lengths, and new_n_free may be n_free; no other two of the buffers may overlap.
  * All device int32: lengths, added, new_lengths, first_row [batch], row_start [batch + 1], table [batch][width], free_pages [cap_free], n_free and
- * new_n_free [1], slots [n_slots] (NULL if n_slots is 0; rows beyond n_slots have no slot written).  A negative length counts as none, a length beyond the table
- * as a full one.  batch <= 65535, width * page_rows < 2^31, and so the sum of the positive changes.
+ * new_n_free [1], slots [n_slots] (NULL if n_slots is 0; rows beyond n_slots have no slot written; row starts stop at 2^31 - 1).  A negative length counts as none, a length beyond the table
+ * as a full one.  batch <= 65535, width * page_rows < 2^31.
  */
 VECTOR_API vector_status vector_block_tables(int32_t batch, const int32_t* lengths, const int32_t* added, int32_t page_rows,
                                              int32_t* table, int32_t width, int32_t* free_pages, int32_t cap_free, const int32_t* n_free,
@@ -421,6 +421,10 @@ VECTOR_API size_t vector_decode_q4_workspace_bytes(const vector_shape* shape);
 /*
  * vector_decode_attn (mode 0) over the paged cache: each sequence attends to its own ret_len and apx_len rows, read on the device, so that a captured call
  * follows them.  A sequence with no rows gives zeros; an entry of a table outside its pool stands for rows that are not there.
+ * Arithmetic: products of stored rows are exact, sums fp32.  The softmax weights enter their products in fp16 (eleven bits; the sum of the weights is of the
+ * same rounded numbers), a key turned back (rope) too; with fp32 queries or fp32 output in two fp16 parts each, and fp32 queries in two.  The key sums, and an fp32
+ * map, keep 24 bits on their way through the map.
+ * ws: at least vector_decode_q4_workspace_bytes() at a multiple of 256 bytes; calls that overlap on the GPU need workspaces of their own.
  * q: device [U][g][d] of shape->dtype; W: device [L * Hkv][d][d]; out: device [U][g][d] of out_dtype.
  */
 VECTOR_API vector_status vector_decode_attn_q4(const vector_shape* shape, const void* q, const vector_q4_cache* cache, const void* W,

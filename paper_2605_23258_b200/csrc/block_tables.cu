@@ -58,6 +58,9 @@ __device__ __forceinline__ int64_t scan(int64_t x, int64_t* warps, int64_t& tota
     return s - x + (wid ? before : 0);
 }
 
+// A sum as a start: what is beyond 2^31 - 1 stays there, behind every slot and page that there can be.
+__device__ __forceinline__ int32_t start_of(int64_t sum) { return (int32_t)min(sum, (int64_t)0x7fffffff); }
+
 // The request that row k of the added rows belongs to: the last b in [lo, hi) with start[b] <= k.
 __device__ __forceinline__ int request_of(const int32_t* start, int lo, int hi, int64_t k) {
     while (hi - lo > 1) {
@@ -117,7 +120,7 @@ block_tables_plan(Args a) {
         if (b < a.batch) c = change_of(a, b);
         const int back = max(c.have - c.want, 0);
         if (!__syncthreads_or(back > 0)) continue;
-        starts[t] = (int32_t)scan(back, warps, total);
+        starts[t] = start_of(scan(back, warps, total));
         first[t] = c.want;
         __syncthreads();
         move_pages(a, b0, n, (int)min(total, (int64_t)a.cap_free - height), starts, first, [&](const int32_t* entry, int) { return *entry; },
@@ -139,7 +142,7 @@ block_tables_plan(Args a) {
         if (__syncthreads_or(need > 0)) {
             const int64_t mine = scan(need, warps, total);
             before += mine;
-            starts[t] = (int32_t)mine;
+            starts[t] = start_of(mine);
             first[t] = c.have;
             __syncthreads();
             const int64_t top = height - 1 - needed;
@@ -150,14 +153,14 @@ block_tables_plan(Args a) {
         }
         if (b < a.batch) {
             const int got = (int)min((int64_t)need, max(height - before, (int64_t)0));
-            const int32_t s = (int32_t)min(start, (int64_t)0x7fffffff), rows = (int32_t)(grow > 0 ? min(c.rows, (int64_t)(c.have + got) * a.page_rows) : c.rows);
+            const int32_t s = start_of(start), rows = (int32_t)(grow > 0 ? min(c.rows, (int64_t)(c.have + got) * a.page_rows) : c.rows);
             a.first_row[b] = (int32_t)c.old_rows;
             a.row_start[b] = s;
             a.new_lengths[b] = rows;
         }
     }
     if (t == 0) {
-        a.row_start[a.batch] = (int32_t)min(added, (int64_t)0x7fffffff);
+        a.row_start[a.batch] = start_of(added);
         a.new_n_free[0] = (int32_t)(height - min(needed, height));
     }
 }
@@ -177,9 +180,14 @@ block_tables_batch(Args a, int parts, int small) {
     if (t < a.batch) { c = change_of(a, t); grow = a.added[t]; }
     const int back = max(c.have - c.want, 0), need = max(c.want - c.have, 0);
     int64_t total, backs = 0, before_back = 0;
-    // rows and pages wanted in one sum: pages are no more than rows, and rows below 2^31
-    const int64_t both = scan(((int64_t)max(grow, 0) << 32) | (uint32_t)need, warps, total);
-    const int64_t rows = total >> 32, needs = (int64_t)(uint32_t)total, start = both >> 32, before = (int64_t)(uint32_t)both;
+    int64_t rows, needs, start, before;
+    if (!__syncthreads_or(grow >= 1 << 21 || need >= 1 << 21)) {      // rows and pages wanted in one sum: THREADS of them stay below 2^31
+        const int64_t both = scan(((int64_t)max(grow, 0) << 32) | (uint32_t)need, warps, total);
+        rows = total >> 32; needs = (int64_t)(uint32_t)total; start = both >> 32; before = (int64_t)(uint32_t)both;
+    } else {
+        start = scan(max(grow, 0), warps, rows);
+        before = scan(need, warps, needs);
+    }
     if (__syncthreads_or(back > 0)) before_back = scan(back, warps, backs);
     const int64_t height = min(n_free + backs, (int64_t)a.cap_free), pops = min(needs, height), pushes = height - n_free;
     const int got = (int)min((int64_t)need, max(height - before, (int64_t)0));
@@ -187,16 +195,16 @@ block_tables_batch(Args a, int parts, int small) {
     if (small && blockIdx.x == 0) {
         if (t < a.batch) {
             a.first_row[t] = (int32_t)c.old_rows;
-            a.row_start[t] = (int32_t)start;
+            a.row_start[t] = start_of(start);
             a.new_lengths[t] = now;
         }
         if (t == 0) {
-            a.row_start[a.batch] = (int32_t)rows;
+            a.row_start[a.batch] = start_of(rows);
             a.new_n_free[0] = (int32_t)(height - pops);
         }
     }
     if (!parts) return;
-    row_start[t] = (int32_t)start; need_start[t] = (int32_t)before; back_start[t] = (int32_t)before_back;
+    row_start[t] = start_of(start); need_start[t] = start_of(before); back_start[t] = start_of(before_back);
     olds[t] = (int32_t)c.old_rows; news[t] = now; haves[t] = c.have; wants[t] = c.want;
     __syncthreads();
     auto released = [&](int64_t e) {                             // the e-th released page

@@ -339,7 +339,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 127);
         const float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
-        const float down = scale_log2e * __uint_as_float((uint32_t)(max(127 - 7 + e, 1)) << 23);
+        const float down = fmaxf(scale_log2e * __uint_as_float((uint32_t)(max(127 - 7 + e, 1)) << 23), 1.2e-38f);      // above zero: a masked logit stays -inf
         fac[0] = __shfl_sync(0xffffffffu, down, (2 * tig) * 4);
         fac[1] = __shfl_sync(0xffffffffu, down, (2 * tig + 1) * 4);
 #pragma unroll

@@ -285,6 +285,7 @@ extern "C" vector_status vector_compact_q4(const vector_shape* shape, const vect
     if (budget->n_apx > 0 && (!apx_idx || !apx_slots || !cache->apx_pages)) return VECTOR_ERR_NULL;
     if (((uintptr_t)K | (uintptr_t)V) & 15) return VECTOR_ERR_SHAPE;
     if (2 * budget->n_ret + budget->n_apx == 0) return VECTOR_OK;
+    if (2 * budget->n_ret + budget->n_apx > (int64_t(1) << 30)) return VECTOR_ERR_SHAPE;
     return q4::by_type(dm, q4::CompactCall{dm, budget, K, V, ret_idx, apx_idx, ret_slots, apx_slots, q4::pools_of(dm, cache), (cudaStream_t)stream});
 }
 
@@ -306,7 +307,7 @@ extern "C" vector_status vector_read_q4(const vector_shape* shape, const vector_
     vector_status rc = check_shape(shape, &dm);
     if (rc != VECTOR_OK) return rc;
     if ((rc = check_q4_cache(cache)) != VECTOR_OK) return rc;
-    if (n_ret < 0 || n_apx < 0 || n_ret > (int64_t(1) << 29) || n_apx > (int64_t(1) << 29)) return VECTOR_ERR_SHAPE;
+    if (n_ret < 0 || n_apx < 0 || n_ret > (int64_t(1) << 30) || n_apx > (int64_t(1) << 30) || 2 * n_ret + n_apx > (int64_t(1) << 30)) return VECTOR_ERR_SHAPE;
     if (n_ret > 0 && (!ret_slots || !ret_k || !ret_v || !cache->ret_pages)) return VECTOR_ERR_NULL;
     if (n_apx > 0 && (!apx_slots || !apx_k || !cache->apx_pages)) return VECTOR_ERR_NULL;
     if (((uintptr_t)ret_k | (uintptr_t)ret_v | (uintptr_t)apx_k) & 15) return VECTOR_ERR_SHAPE;

@@ -98,3 +98,14 @@ def test_a_captured_step_follows_its_lengths():
         new, old, t, s, h, st, sl = plain.tables(state[0], added.tolist(), page, state[1], state[2], state[3])
         assert (lengths.tolist(), first.tolist(), table.tolist(), stack.tolist(), n_free.item(), start.tolist(), slots.tolist()) == (new, old, t, s, h, st, (sl + [-1] * B)[:B])
         state = [new, t, s, h]
+
+
+@pytest.mark.parametrize("B", [6, 1500])
+def test_changes_whose_sum_is_beyond_31_bits(B):
+    """Requests that ask for all there could be: pages go as far as they go, sums stop at 2^31 - 1."""
+    lengths, added = np.zeros(B, int), np.full(B, 2**31 - 1)
+    table, stack = np.full((B, 3), -1), np.arange(10)
+    new, first, T, F, left, start, slots = _run(lengths, added, 4, table, stack, 10, 40)
+    assert new.tolist() == [12, 12, 12, 4] + [0] * (B - 4) and left.tolist() == [0]
+    assert T[:4].tolist() == [[9, 8, 7], [6, 5, 4], [3, 2, 1], [0, -1, -1]] and start[:3].tolist() == [0, 2**31 - 1, 2**31 - 1]
+    assert slots.tolist() == [p * 4 + r for p in (9, 8, 7) for r in range(4)] + [-1] * 28

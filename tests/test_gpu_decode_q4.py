@@ -112,3 +112,51 @@ def test_large_queries_and_keys():
     keys = plain.row_values(c.ret_pages.cpu().numpy(), plain.slots_of(c.ret_table[0].cpu().numpy(), 80), 0, 0, 128)
     best = (q[0].double().cpu().numpy() @ keys.T).argmax(-1)
     assert abs(out[0].double().cpu().numpy() - rows[best]).max() <= 2.0 ** -20 * abs(rows).max()
+
+
+def test_the_largest_batch():
+    """1024 sequences, a few rows each, most places empty; one more is refused."""
+    lengths = [(i % 7, (i * 5) % 11) if i % 3 == 0 else (0, 0) for i in range(1024)]
+    lengths[1023] = (200, 129)
+    p = plain.problem(1024, 1, 1, 2, 64, BF, lengths, 13)
+    out = plain.decode(*p, F32)
+    plain.check_decode(*p, out, False, [0, 3, 999, 1020, 1022, 1023])
+    assert not out[1::3].any() and not out[2::3].any()
+
+
+def test_offsets_beyond_32_bits():
+    """Pages beyond 4 GB of both pools, written, read back and attended to."""
+    import numpy as np
+    sh = vec.Shape(1, 1, 4, 1, 128, vec.VECTOR_BF16, 16)
+    pages = (1 << 32) // 4608 + 20
+    c = vec.alloc_q4_cache(sh, pages, pages, 2, 2, positions=False)
+    rng = np.random.default_rng(2)
+    budget = vec.vector_plan_budget(200, 100, 30, 16)                            # 70 retained, 60 key-only
+    K, V = (torch.from_numpy(rng.standard_normal((1, 200, 128))).to(BF).cuda() for _ in range(2))
+    idx = torch.from_numpy(rng.permutation(200)[:130].astype(np.int32)).cuda()
+    ret, apx = idx[:70].sort().values[None].contiguous(), idx[70:].sort().values[None].contiguous()
+    c.ret_table[0] = torch.tensor([pages - 1, 0])
+    c.apx_table[0] = torch.tensor([pages - 2, pages - 1])
+    c.ret_len[0], c.apx_len[0] = 70, 60
+    rs, as_ = (torch.from_numpy(plain.slots_of(t[0].cpu().numpy(), n)[None].astype(np.int32)).cuda() for t, n in ((c.ret_table, 70), (c.apx_table, 60)))
+    vec.vector_compact_q4(sh, budget, K, V, ret, apx, c, rs, as_)
+    got = [torch.empty(1, n, 128, dtype=BF, device="cuda") for n in (70, 70, 60)]
+    vec.vector_read_q4(sh, c, rs, got[0], got[1], as_, got[2])
+    torch.cuda.synchronize()
+    want = [plain.rounded(x[0].double().cpu().numpy()[i[0].long().cpu().numpy()]) for x, i in ((K, ret), (V, ret), (K, apx))]
+    for x, w in zip(got, want):
+        assert np.array_equal(x[0].double().cpu().numpy(), w)
+    q, W = torch.randn(1, 4, 128, device="cuda").to(BF), (torch.randn(1, 128, 128, device="cuda") / 11).to(BF)
+    out = plain.decode(sh, q, c, W, F32)
+    o, *sizes = plain.attend(q[0].double().cpu().numpy(), *want, W[0].double().cpu().numpy(), 128 ** -0.5)
+    assert np.all(np.abs(out[0].double().cpu().numpy() - o) <= plain.tolerance(o, *sizes, BF, F32, False))
+
+
+def test_scales_of_logits_near_nothing():
+    """A logit scale at the end of fp32's range: all weights are alike, and rows that are not there still have none."""
+    sh, q, c, W = plain.problem(1, 1, 1, 2, 128, BF, [(70, 0)], 14)
+    sh.sm_scale = 1e-38
+    out = plain.decode(sh, q, c, W, F32)
+    import numpy as np
+    rows = plain.row_values(c.ret_pages.cpu().numpy(), plain.slots_of(c.ret_table[0].cpu().numpy(), 70), 0, 1, 128)
+    assert abs(out[0].double().cpu().numpy() - rows.mean(0)).max() <= 2.0 ** -20 * np.abs(rows).mean(0).max()
