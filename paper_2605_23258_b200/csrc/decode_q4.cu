@@ -43,14 +43,12 @@ struct Call {
                                               dm.g, seqs, (const T*)W, out, out_dtype == VECTOR_BF16 ? 1 : 0));
         return VECTOR_OK;
     }
-    // A unit a multiprocessor: a large block a unit, since the records are many.  More: small blocks, and as many sequences for a fetched map as leave a round of blocks.
+    // No more units than multiprocessors: a large block a unit, since a unit's records are many then (8 units of 39 records, attention in all: 15.8 us, by blocks of 256
+    // threads 23.5).  More: small blocks, and as many sequences for a map that is fetched once as leave one round of blocks (2048 units of eight sequences and
+    // one tile: 25.1 us, a unit a block 26.7; of 28 tiles 132.0 and 132.3).
     template <typename T, int D, int HP> vector_status merge_heads() const {
         if (dm.U <= sm_count()) return merge_by<T, D, HP, MERGE_MOST>(1);
-#ifndef DQ4_S
         const int resident = (sizeof(T) == 2 ? 4 : 3) * sm_count(), rounds = (dm.U + resident - 1) / resident;
-#else
-        const int rounds = DQ4_S;
-#endif
         return merge_by<T, D, HP, MERGE_THREADS>(rounds < c.batch ? rounds : c.batch);
     }
     template <typename T, int D> vector_status merge() const {
