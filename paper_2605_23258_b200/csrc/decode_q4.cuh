@@ -6,7 +6,7 @@
 // unit's tier and writes it as a partial record when it leaves that.  The lengths lie on the device, so every block sums up the
 // sequences' costs itself.
 //
-// A worker takes 32 keys at a time.  A stored row's piece t is what lane t of a quad holds of a 16 x 16 fragment whose rows are keys: one 16-byte load (8 for
+// A worker takes 16 or 32 keys at a time.  A stored row's piece t is what lane t of a quad holds of a 16 x 16 fragment whose rows are keys: one 16-byte load (8 for
 // 64 channels) of codes and two scales a row, one conversion and one product for two channels, and no exchange between lanes:
 //   S^T = K Q^T    m16n8k16, keys down, the query heads across: no padding to sixteen rows of queries
 //   softmax        in fp32, against a reference that follows the maximum only when that has moved by more than SLACK (powers of two); the weights go to fp16
@@ -14,10 +14,11 @@
 //                  A^T += K^T P^T of key-only keys, from the very registers that gave the logits
 // The sum of the weights is one more row of that product, a row of ones, so that a weight's rounding to fp16 is in numerator and denominator alike.
 // Stored rows are exact in fp16, so the products are.  Queries are scaled by a power of two a head to fp16's range; fp32 queries take two fp16 parts.
-// EXACT (fp32 queries or fp32 output): weights, and keys turned back, in two fp16 parts, and sums of 32 keys added up outside the tensor cores,
+// EXACT (fp32 queries or fp32 output): weights, and keys turned back, in two fp16 parts, and sums of 16 keys added up outside the tensor cores,
 // which cut their sums off instead of rounding them.
 //
-// Merge kernel.  A block per unit combines its records, applies the map to the key sums on the tensor cores (in three bf16 parts: 24 bits) and normalises.
+// Merge kernel.  A block combines the records of a unit, or of several sequences' units of one (layer, KV head), applies the map to the key sums on the
+// tensor cores (in three bf16 parts: 24 bits) and normalises.
 #ifndef VECTOR_DECODE_Q4_CUH_
 #define VECTOR_DECODE_Q4_CUH_
 
