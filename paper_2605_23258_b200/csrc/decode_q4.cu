@@ -29,9 +29,9 @@ struct Call {
         if (ROPE) rope_phases(dm.theta, D, &ph);
         VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::SMEM_BYTES + (size_t)(c.batch + 1) * 8, st, (const T*)q, c, dm.g,
                                               dm.scale * 1.4426950408889634f, ws, fault, ph));
-        return merge<T, D>();
+        return merge<T, D>(sm_count() * C::WARPS);
     }
-    template <typename T, int D, int HP, int THREADS> vector_status merge_by(int seqs) const {
+    template <typename T, int D, int HP, int THREADS> vector_status merge_by(int seqs, int workers) const {
         auto kern = decode_q4_merge<T, D, HP, THREADS>;
         constexpr int smem = MapTile<T, D>::BYTES;
         static PerDeviceOnce once;
@@ -40,19 +40,19 @@ struct Call {
             if (e != cudaSuccess) { once.undo(); VEC_CUDA_CHECK(e); }
         }
         VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3((unsigned)(dm.LH * ((c.batch + seqs - 1) / seqs))), dim3(THREADS), smem, st, (const unsigned char*)ws, c,
-                                              dm.g, seqs, (const T*)W, out, out_dtype == VECTOR_BF16 ? 1 : 0));
+                                              dm.g, seqs, workers, (const T*)W, out, out_dtype == VECTOR_BF16 ? 1 : 0));
         return VECTOR_OK;
     }
     // No more units than multiprocessors: a large block a unit, since a unit's records are many then (8 units of 39 records, attention in all: 15.8 us, by blocks of 256
     // threads 23.5).  More: small blocks, and as many sequences for a map that is fetched once as leave one round of blocks (2048 units of eight sequences and
     // one tile: 25.1 us, a unit a block 26.7; of 28 tiles 132.0 and 132.3).
-    template <typename T, int D, int HP> vector_status merge_heads() const {
-        if (dm.U <= sm_count()) return merge_by<T, D, HP, MERGE_MOST>(1);
+    template <typename T, int D, int HP> vector_status merge_heads(int workers) const {
+        if (dm.U <= sm_count()) return merge_by<T, D, HP, MERGE_MOST>(1, workers);
         const int resident = (sizeof(T) == 2 ? 4 : 3) * sm_count(), rounds = (dm.U + resident - 1) / resident;
-        return merge_by<T, D, HP, MERGE_THREADS>(rounds < c.batch ? rounds : c.batch);
+        return merge_by<T, D, HP, MERGE_THREADS>(rounds < c.batch ? rounds : c.batch, workers);
     }
-    template <typename T, int D> vector_status merge() const {
-        return dm.g <= 2 ? merge_heads<T, D, 1>() : dm.g <= 4 ? merge_heads<T, D, 2>() : dm.g <= 6 ? merge_heads<T, D, 3>() : merge_heads<T, D, 4>();
+    template <typename T, int D> vector_status merge(int workers) const {
+        return dm.g <= 2 ? merge_heads<T, D, 1>(workers) : dm.g <= 4 ? merge_heads<T, D, 2>(workers) : dm.g <= 6 ? merge_heads<T, D, 3>(workers) : merge_heads<T, D, 4>(workers);
     }
     template <typename T, int D> vector_status run() const {
         const bool exact = dm.dtype == VECTOR_F32 || out_dtype == VECTOR_F32;

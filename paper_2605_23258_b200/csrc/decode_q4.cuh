@@ -51,6 +51,9 @@ __device__ __forceinline__ int tiles_of(int rows) { return (rows + q4::ROWS - 1)
 
 // ---- workspace: the first and the last worker of every unit that has tiles, then the records
 __host__ __device__ inline size_t ends_bytes(int units) { return ((size_t)units * 8 + 255) & ~(size_t)255; }
+// Whether a unit's ends are what workers wrote.  They are not where a streaming warp's wait gave up before it got there: then they are whatever the workspace
+// held, and no record's address may come from them.
+__host__ __device__ constexpr bool ends_are_workers(int first, int last, int workers) { return first >= 0 && first <= last && last < workers; }
 // A record: for each tier [heads, rounded up to even][m, l] and the sums, in the order of the fragments.
 __host__ __device__ inline int even_heads(int g) { return (g + 1) & ~1; }
 __host__ __device__ inline int tier_floats(int g, int d) { return even_heads(g) * (d + 2); }
@@ -660,10 +663,10 @@ template <typename T, int D> struct MapTile {
 };
 
 // The records of `seqs` sequences' units of one (layer, KV head) into their outputs: the map is fetched once for all of them.
-// HP: pairs of heads.
+// HP: pairs of heads; workers: of the streaming kernel.
 template <typename T, int D, int HP, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == MERGE_MOST ? 1 : sizeof(T) == 2 ? 4 : 3)
-decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, const T* W, void* __restrict__ out, int out_bf16) {
+decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, int workers, const T* W, void* __restrict__ out, int out_bf16) {
     constexpr int NW = THREADS / 32, GROUPS = THREADS / MERGE_THREADS, ROWS_W = 16, heads = 2 * HP;
     // Four numbers of a tier's sums are a thread's, ROUNDS times at the most: rows `row` and `row` + 8 of O tile t, heads 2 hp and 2 hp + 1.
     constexpr int quads = D / 16 * HP * 8, ROUNDS = (2 * quads + MERGE_THREADS - 1) / MERGE_THREADS;
@@ -692,6 +695,10 @@ decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, const T* W, v
         const size_t o = (size_t)u * g * D;
         if (n_ret + n_apx == 0) {                                     // nothing to attend to, and no record
             for (int e = threadIdx.x; e < g * D; e += THREADS) put_out(o + e, 0.f);
+            continue;
+        }
+        if (!ends_are_workers(ends.x, ends.y, workers)) {
+            for (int e = threadIdx.x; e < g * D; e += THREADS) put_out(o + e, __int_as_float(0x7fffffff));
             continue;
         }
         const int pieces = ends.y - ends.x + 1;                       // the unit's own record, then those of the workers behind its first
