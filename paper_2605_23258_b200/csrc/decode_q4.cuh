@@ -636,6 +636,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
 // Threads of a merge block, which takes the records of a unit in groups of MERGE_THREADS, each a part of the records.
 constexpr int MERGE_THREADS = 256, MERGE_MOST = 1024;
 constexpr int MERGE_CHUNK = 64;      // records of a unit that are weighed at a time
+constexpr float EMPTY = -1.f;        // in place of the factor of a record without rows
 
 // The map in shared memory, its 16-byte pieces so that a fragment's rows do not meet in a bank: pieces of odd rows change places.
 template <typename T, int D> struct MapTile {
@@ -729,10 +730,13 @@ decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, int workers, 
                 for (int i = lane; i < 2 * n; i += 32) M = fmaxf(M, ml[i >> 1][i & 1][h].x);
                 M = warp_max(M);
                 float L = 0.f;
+                // An empty record has no sum either, and its numbers are not any.  One of logits that are all NaN has no reference, but a sum, which is NaN: its factor is
+                // zero or NaN, its numbers count.  So does one whose factor is zero because its logits are small.
                 for (int i = lane; i < 2 * n; i += 32) {
                     const float2 x = ml[i >> 1][i & 1][h];
-                    const float f = x.x == -INFINITY ? 0.f : exp2f(x.x - M);      // an empty record's sum and numbers are not any
-                    if (f != 0.f) L = fmaf(f, x.y, L);
+                    const bool empty = x.x == -INFINITY && x.y == 0.f;
+                    const float f = empty ? EMPTY : exp2f(x.x - M);
+                    if (!empty) L = fmaf(f, x.y, L);
                     fac[i & 1][h][i >> 1] = f;
                 }
                 L = warp_sum(L);
@@ -759,7 +763,7 @@ decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, int workers, 
                     for (int z = 0; z < UN; ++z) {
                         if (at + z * GROUPS >= n) break;
                         const float x0 = f0[at + z * GROUPS], x1 = f1[at + z * GROUPS];
-                        if (x0 == 0.f && x1 == 0.f) continue;
+                        if (x0 == EMPTY) continue;                     // then so is x1: a tier of a record is empty for all heads
                         a[j].x = fmaf(x0, w[z].x, a[j].x); a[j].y = fmaf(x1, w[z].y, a[j].y); a[j].z = fmaf(x0, w[z].z, a[j].z); a[j].w = fmaf(x1, w[z].w, a[j].w);
                     }
                 }
