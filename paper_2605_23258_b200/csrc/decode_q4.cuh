@@ -134,7 +134,13 @@ __device__ __forceinline__ uint32_t neg_h2(uint32_t a) {
     asm("neg.f16x2 %0, %1;\n" : "=r"(r) : "r"(a));
     return r;
 }
+// Infinities stay: an infinite query's logits are none.
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_h2_cut(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
@@ -492,9 +498,9 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                     auto parts = [](uint64_t z, uint32_t& hi, uint32_t& low) {
                         float a, b;
                         tc::unpack2(z, a, b);
-                        hi = pack_h2(a, b);
+                        hi = pack_h2_cut(a, b);
                         const float2 f = unpack_h2(hi);
-                        low = pack_h2(a - f.x, b - f.y);
+                        low = pack_h2_cut(a - f.x, b - f.y);
                     };
                     parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
                     parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);

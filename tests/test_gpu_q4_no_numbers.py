@@ -20,7 +20,7 @@ def _spoil(c, tier, d, b, row, which=0):
 
 @pytest.mark.parametrize("rope", [False, True])
 @pytest.mark.parametrize("dtype,out_dtype", TYPES)
-@pytest.mark.parametrize("d,g,value", [(128, 3, float("nan")), (64, 2, float("nan")), (128, 8, float("nan"))])
+@pytest.mark.parametrize("d,g,value", [(128, 3, float("nan")), (64, 2, float("nan")), (128, 8, float("nan")), (128, 3, float("inf")), (64, 5, float("-inf"))])
 def test_a_query_that_is_none(dtype, out_dtype, d, g, value, rope):
     sh, q, c, W = plain.problem(3, 1, 1, g, d, dtype, [(70, 130), (3, 0), (0, 65)], 41, rope)
     q[:, 1, d // 2 + 3] = value
