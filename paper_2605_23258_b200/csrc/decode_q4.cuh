@@ -13,7 +13,7 @@
 //   O^T += V^T P^T channels down, heads across; both operands are the registers at hand after an 8 x 8 transpose (movmatrix), and so are the key sums
 //                  A^T += K^T P^T of key-only keys, from the very registers that gave the logits
 // The sum of the weights is one more row of that product, a row of ones, so that a weight's rounding to fp16 is in numerator and denominator alike.
-// Stored rows are exact in fp16, so the products are.  Queries are scaled by a power of two a head to fp16's range; fp32 queries take two fp16 parts.
+// Stored rows are exact in fp16, so the products are; halves of them too.  Queries are scaled by a power of two a head to fp16's range; fp32 queries take two fp16 parts.
 // EXACT (fp32 queries or fp32 output): weights, and keys turned back, in two fp16 parts, and sums of 16 keys added up outside the tensor cores,
 // which cut their sums off instead of rounding them.
 //
@@ -93,6 +93,8 @@ template <typename T, int D, bool ROPE, bool EXACT, bool FOLD> struct Cfg {
     static constexpr int ENTRY_BYTES = q4::Row<D>::TILE + (ROPE ? 4 * q4::ROWS : 0);
     static constexpr int SMEM_BYTES = WARPS * ENTRIES * ENTRY_BYTES;   // and behind them the prefix sums
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
+    // Rows that may be turned are taken halved: a pair of stored channels, 61440 each, turns to 86889 at the most, and half of that is within fp16's 65504.
+    static constexpr float ROW_UNIT = ROPE ? .5f : 1.f;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
     // Rows of a softmax step, in sixteens.  us by (retained, key-only): 640 units of 3300 and 6550 rows (2, 1) 181, (1, 1) 181, (2, 2) 187; 2048 units of 650 and 1120 rows
@@ -138,11 +140,6 @@ __device__ __forceinline__ uint32_t neg_h2(uint32_t a) {
 __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
     uint32_t r;
     asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
-    return r;
-}
-__device__ __forceinline__ uint32_t pack_h2_cut(float lo, float hi) {
-    uint32_t r;
-    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
@@ -349,7 +346,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 127);
         const float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
-        const float down = fmaxf(scale_log2e * __uint_as_float((uint32_t)(max(127 - 7 + e, 1)) << 23), 1.2e-38f);      // above zero: a masked logit stays -inf
+        const float down = fmaxf(scale_log2e / C::ROW_UNIT * __uint_as_float((uint32_t)(max(127 - 7 + e, 1)) << 23), 1.2e-38f);      // above zero: a masked logit stays -inf
         fac[0] = __shfl_sync(0xffffffffu, down, (2 * tig) * 4);
         fac[1] = __shfl_sync(0xffffffffu, down, (2 * tig + 1) * 4);
 #pragma unroll
@@ -363,7 +360,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             }
         }
     };
-    // Rows row0 + gid and row0 + gid + 8 of a tile as A fragments.
+    // Rows row0 + gid and row0 + gid + 8 of a tile as A fragments, times ROW_UNIT (exact: nothing stored is below 2^-18).
     auto load_rows = [&](const unsigned char* tile, int row0, uint32_t (&x)[2][C::PAIRS]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -377,7 +374,10 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 w[0] = v.x; w[1] = v.y;
             }
             const unsigned char* s = tile + R::SCALES_AT + row * R::GROUPS + 2 * (D == 128 ? tig : tig >> 1);
-            const uint32_t s2[2] = {s[0] * 0x00800080u, s[1] * 0x00800080u};
+            uint32_t s2[2] = {s[0] * 0x00800080u, s[1] * 0x00800080u};
+            if constexpr (ROPE)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) s2[i] = mul_h2(s2[i], 0x38003800u);
 #pragma unroll
             for (int j = 0; j < D / 32; ++j) {
                 uint32_t p[4];
@@ -498,9 +498,9 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                     auto parts = [](uint64_t z, uint32_t& hi, uint32_t& low) {
                         float a, b;
                         tc::unpack2(z, a, b);
-                        hi = pack_h2_cut(a, b);
+                        hi = pack_h2(a, b);
                         const float2 f = unpack_h2(hi);
-                        low = pack_h2_cut(a - f.x, b - f.y);
+                        low = pack_h2(a - f.x, b - f.y);
                     };
                     parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
                     parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);
@@ -535,7 +535,10 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         if (empty) return;
         float4* o = reinterpret_cast<float4*>(p + 2 * heads);
 #pragma unroll
-        for (int t = 0; t < C::O_TILES; ++t) o[(t * (heads / 2) + tig) * 8 + gid] = make_float4(O[t][0], O[t][1], O[t][2], O[t][3]);
+        for (int t = 0; t < C::O_TILES; ++t) {
+            constexpr float back = 1.f / C::ROW_UNIT;
+            o[(t * (heads / 2) + tig) * 8 + gid] = make_float4(O[t][0] * back, O[t][1] * back, O[t][2] * back, O[t][3] * back);
+        }
     };
     auto leave_unit = [&] {
         if (unit < 0) return;
