@@ -196,11 +196,19 @@ template <typename Cost> struct Runs {
 enum Kind { KEYS, VALUES, KEY_ONLY };
 struct Entry { int unit, rows, kind, edge; };
 
-// Sine and cosine of an angle in 2^-32 turns, by its upper 23 bits (8e-7): they become a number in [1, 2) and that a multiple of 2 pi
-// about zero, without a conversion from integers, which would wait for the unit that the sine and the cosine keep busy.
-__device__ __forceinline__ void turn_cos_sin(uint32_t angle, float& cs, float& sn) {
-    const float turns = __uint_as_float((angle >> 9) ^ 0x3fc00000u);         // 1 + (angle + half a turn) modulo a turn
-    __sincosf(fmaf(turns, 6.283185307179586f, -9.42477796076938f), &sn, &cs);
+// Phases of two neighbouring channel pairs, turns a position: multiples of 2^-32, and what these leave, in radians.
+struct __align__(16) TwoPhases { uint32_t turns[2]; float rest[2]; };
+__device__ __forceinline__ void put_phase(TwoPhases* to, int channel, unsigned long long phase) {
+    const uint32_t turns = (uint32_t)((phase + 0x80000000ull) >> 32);
+    to[channel / 2].turns[channel % 2] = turns;
+    to[channel / 2].rest[channel % 2] = (float)(int32_t)(uint32_t)phase * 3.4061215800865545e-19f;      // 2 pi / 2^64
+}
+// Sine and cosine of a position times a phase.  Of the product modulo a turn the upper 23 bits count (8e-7): they become a number in [1, 2) and that a multiple of 2 pi
+// about zero, without a conversion from integers, which would wait for the unit that the sine and the cosine keep busy.  The phase's rest, under 2^-33 of a turn a position,
+// comes on top: 1e-4 at position 131072, 0.8 at 2^30 (16 sequences of 3000 and 6000 rows in 8 heads: 70.4 us, without it 67; by an integer product in its place 72.6).
+__device__ __forceinline__ void turn_cos_sin(uint32_t pos, float pos_f, uint32_t phase, float rest, float& cs, float& sn) {
+    const float turns = __uint_as_float(((pos * phase) >> 9) ^ 0x3fc00000u);         // 1 + (angle + half a turn) modulo a turn
+    __sincosf(fmaf(turns, 6.283185307179586f, fmaf(pos_f, rest, -9.42477796076938f)), &sn, &cs);
 }
 // N neighbouring numbers at a multiple of 16 bytes.
 template <int N> __device__ __forceinline__ void load_run(const float* p, float* x) {
@@ -230,7 +238,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     __shared__ __align__(8) uint64_t full[WARPS][ENTRIES];
     __shared__ Entry entries[WARPS][ENTRIES];
     __shared__ int64_t sums[WARPS];
-    __shared__ __align__(8) uint32_t phase32[ROPE ? D / 2 : 1];
+    __shared__ TwoPhases phase32[ROPE && !EXACT ? D / 4 : 1];
     __shared__ RopePhase phase64[ROPE && EXACT ? D / 2 : 1];
     int64_t* prefix = reinterpret_cast<int64_t*>(smem + C::SMEM_BYTES);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, gid = lane >> 2, tig = lane & 3;
@@ -241,8 +249,8 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     }
     if constexpr (ROPE) {
         if (threadIdx.x < D / 2) {
-            phase32[threadIdx.x] = (uint32_t)((phases.phase[threadIdx.x] + 0x80000000ull) >> 32);
             if constexpr (EXACT) phase64[threadIdx.x] = rope_phase_words(phases.phase[threadIdx.x]);
+            else put_phase(phase32, threadIdx.x, phases.phase[threadIdx.x]);
         }
     }
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
@@ -505,10 +513,11 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                     parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
                     parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);
                 } else {
-                    const uint2 ph2 = *reinterpret_cast<const uint2*>(&phase32[ch]);
+                    const TwoPhases two = phase32[ch / 2];
+                    const float at = (float)pos[h];
                     float c0, s0, c1, s1;
-                    turn_cos_sin((uint32_t)pos[h] * ph2.x, c0, s0);
-                    turn_cos_sin((uint32_t)pos[h] * ph2.y, c1, s1);
+                    turn_cos_sin((uint32_t)pos[h], at, two.turns[0], two.rest[0], c0, s0);
+                    turn_cos_sin((uint32_t)pos[h], at, two.turns[1], two.rest[1], c1, s1);
                     const uint32_t cs = pack_h2(c0, c1), sn = pack_h2(s0, s1), a = u, b = v;
                     u = fma_h2(a, cs, mul_h2(b, sn));
                     v = fma_h2(neg_h2(a), sn, mul_h2(b, cs));

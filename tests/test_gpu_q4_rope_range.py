@@ -1,4 +1,4 @@
-"""Rotary keys of the 4-bit paged cache at the ends of what is stored: channels of 61440, whose pairs turn to 86889."""
+"""Rotary keys of the 4-bit paged cache at the ends of what is stored and of the positions: channels of 61440, whose pairs turn to 86889, and far tokens."""
 import numpy as np
 import pytest
 import torch
@@ -36,3 +36,12 @@ def test_the_largest_stored_keys(dtype, out_dtype, d, g):
         tol = plain.tolerance(o, spread, logit * heads.start, turned, dtype, out_dtype, True)
         err = np.abs(out[0, heads].double().cpu().numpy() - o)
         assert np.all(np.isfinite(err)) and np.all(err <= tol), (heads.start, float((err / tol).max()))
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("d,g,top", [(128, 4, 1 << 20), (64, 3, 1 << 30), (128, 2, 1 << 30)])
+def test_far_positions(dtype, out_dtype, d, g, top):
+    """Positions up to 2^30: the tolerance is that of near ones."""
+    sh, q, c, W = plain.problem(2, 1, 1, g, d, dtype, [(0, 200), (90, 65)], 32, rope=True)
+    c.apx_pos.copy_(torch.randint(top // 2, top, c.apx_pos.shape, generator=torch.Generator().manual_seed(1), dtype=torch.int32))
+    plain.check_decode(sh, q, c, W, plain.decode(sh, q, c, W, out_dtype), True)
