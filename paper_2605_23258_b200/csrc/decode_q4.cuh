@@ -9,7 +9,7 @@
 // A worker takes 16 or 32 keys at a time.  A stored row's piece t is what lane t of a quad holds of a 16 x 16 fragment whose rows are keys: one 16-byte load (8 for
 // 64 channels) of codes and two scales a row, one conversion and one product for two channels, and no exchange between lanes:
 //   S^T = K Q^T    m16n8k16, keys down, the query heads across: no padding to sixteen rows of queries
-//   softmax        in fp32, against a reference that follows the maximum only when that has moved by more than SLACK (powers of two); the weights go to fp16
+//   softmax        in fp32, against a reference that follows the maximum only when that has moved by more than SLACK (powers of two); the weights go to fp16, LEAD above one
 //   O^T += V^T P^T channels down, heads across; both operands are the registers at hand after an 8 x 8 transpose (movmatrix), and so are the key sums
 //                  A^T += K^T P^T of key-only keys, from the very registers that gave the logits
 // The sum of the weights is one more row of that product, a row of ones, so that a weight's rounding to fp16 is in numerator and denominator alike.
@@ -37,7 +37,12 @@ namespace dq4 {
 constexpr int MAX_BATCH = VECTOR_Q4_MAX_BATCH;
 // What a tile of either tier costs a worker, in small numbers.
 template <int RET, int APX> struct Costs { static constexpr int ret = RET, apx = APX, most = RET > APX ? RET : APX; };
-constexpr float SLACK = 8.f;
+// A weight is 2^(logit - reference), and the reference is the largest logit so far less LEAD, or up to SLACK below that: weights reach 2^15 of fp16's range.  They have eleven bits
+// down to 2^-14, 2^-27 of the largest, and end at 2^-25, so that thousands of small weights count behind one key that takes nearly all.
+constexpr float LEAD = 13.f, SLACK = 2.f;
+static_assert(LEAD + SLACK <= 15.f, "weights are below 65504");
+// What second parts are multiplied by, which their products' sums give back: they keep eleven bits where they would be subnormal.
+constexpr float PART = 2048.f;
 
 struct Cache {
     const unsigned char *ret, *apx;
@@ -432,12 +437,12 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             for (int i = 1; i < N; ++i) top[h] = fmaxf(top[h], fmaxf(S[i][h], S[i][2 + h]));
             top[h] *= fac[h];
         }
-        if (__any_sync(0xffffffffu, top[0] > m[0] + SLACK || top[1] > m[1] + SLACK)) {
+        if (__any_sync(0xffffffffu, top[0] > m[0] + (LEAD + SLACK) || top[1] > m[1] + (LEAD + SLACK))) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], o));
-                const float now = fmaxf(m[h], top[h]), f = m[h] == now ? 1.f : tc::ex2(m[h] - now);
+                const float now = fmaxf(m[h], top[h] - LEAD), f = m[h] == now ? 1.f : tc::ex2(m[h] - now);
                 m[h] = now;
 #pragma unroll
                 for (int t = 0; t < C::O_TILES; ++t) { O[t][h] *= f; O[t][2 + h] *= f; }
@@ -452,7 +457,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 const uint32_t hi = pack_h2(a, b);
                 if constexpr (EXACT) {
                     const float2 f = unpack_h2(hi);
-                    const uint32_t low = pack_h2(a - f.x, b - f.y);
+                    const uint32_t low = pack_h2((a - f.x) * PART, (b - f.y) * PART);
                     ph[i][h] = transpose(FOLD && tig >= 2 ? low : hi);
                     if constexpr (!FOLD) pl[i][h] = transpose(low);
                 } else {
@@ -468,7 +473,12 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             if constexpr (EXACT) {
                 float sum[4];
                 mma_alone(sum, a0, a1, a2, a3, ph[0], ph[1]);
-                if constexpr (!FOLD) mma(sum, a0, a1, a2, a3, pl[0], pl[1]);
+                if constexpr (!FOLD) {
+                    float second[4];
+                    mma_alone(second, a0, a1, a2, a3, pl[0], pl[1]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) sum[e] = fmaf(second[e], 1.f / PART, sum[e]);
+                }
                 if constexpr (with_lo.value) mma(sum, transpose(lo[0][2 * t]), transpose(lo[0][2 * t + 1]), transpose(lo[1][2 * t]), transpose(lo[1][2 * t + 1]), ph[0], ph[1]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[t][e] += sum[e];
@@ -480,7 +490,11 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         if constexpr (EXACT) {
             float sum[4];
             mma_alone(sum, ONE, ONE, ONE, ONE, ph[0], ph[1]);
-            if constexpr (!FOLD) mma(sum, ONE, ONE, ONE, ONE, pl[0], pl[1]);
+            if constexpr (!FOLD) {
+                float second[4];
+                mma_alone(second, ONE, ONE, ONE, ONE, pl[0], pl[1]);
+                sum[0] = fmaf(second[0], 1.f / PART, sum[0]); sum[1] = fmaf(second[1], 1.f / PART, sum[1]);
+            }
             L[0] += sum[0]; L[1] += sum[1];
         } else {
             mma(L, ONE, ONE, ONE, ONE, ph[0], ph[1]);
@@ -535,9 +549,9 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
 #pragma unroll
                 for (int t = 0; t < C::O_TILES; ++t)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) O[t][e] += __shfl_xor_sync(0xffffffffu, O[t][e], 2);
+                    for (int e = 0; e < 4; ++e) O[t][e] = fmaf(__shfl_xor_sync(0xffffffffu, O[t][e], 2), 1.f / PART, O[t][e]);      // the lower lanes', which hold the first parts
 #pragma unroll
-                for (int h = 0; h < 2; ++h) L[h] += __shfl_xor_sync(0xffffffffu, L[h], 2);
+                for (int h = 0; h < 2; ++h) L[h] = fmaf(__shfl_xor_sync(0xffffffffu, L[h], 2), 1.f / PART, L[h]);
             }
         if (2 * tig >= heads) return;
         if (gid == 0) *reinterpret_cast<float4*>(p + 4 * tig) = empty ? make_float4(-INFINITY, 0.f, -INFINITY, 0.f) : make_float4(m[0], L[0], m[1], L[1]);
