@@ -341,7 +341,8 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         L[0] = L[1] = L[2] = L[3] = 0.f;                               // L: the same sums in all rows, of which two numbers are used
     };
     clear();
-    // The queries of a unit as B fragments: head gid, the channels of piece tig.  Scaled so that the largest lies in [2^7, 2^8).
+    // The queries of a unit as B fragments: head gid, the channels of piece tig.  Scaled so that the largest lies in [2^14, 2^15): channels of 2^-28
+    // of it still have eleven bits.
     auto load_queries = [&](int unit) {
         const int head = FOLD ? gid & 3 : gid;
         const T* row = q + ((size_t)unit * g + min(head, g - 1)) * D + tig * (D / 8);
@@ -358,8 +359,8 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
         const int e = min(max((int)(__float_as_uint(most) >> 23) - 127, -100), 127);
-        const float up = __uint_as_float((uint32_t)(127 + 7 - e) << 23);
-        const float down = fmaxf(scale_log2e / C::ROW_UNIT * __uint_as_float((uint32_t)(max(127 - 7 + e, 1)) << 23), 1.2e-38f);      // above zero: a masked logit stays -inf
+        const float up = __uint_as_float((uint32_t)(127 + 14 - e) << 23);
+        const float down = fmaxf(scale_log2e / C::ROW_UNIT * __uint_as_float((uint32_t)(127 - 14 + e) << 23), 1.2e-38f);      // above zero: a masked logit stays -inf
         fac[0] = __shfl_sync(0xffffffffu, down, (2 * tig) * 4);
         fac[1] = __shfl_sync(0xffffffffu, down, (2 * tig + 1) * 4);
 #pragma unroll
@@ -369,7 +370,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             qb[0][i / 2][i % 2] = hi;
             if constexpr (C::Q_PARTS == 2) {
                 const float2 f = unpack_h2(hi);
-                qb[1][i / 2][i % 2] = pack_h2(a - f.x, b - f.y);
+                qb[1][i / 2][i % 2] = pack_h2((a - f.x) * PART, (b - f.y) * PART);
             }
         }
     };
@@ -416,7 +417,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                     else mma(sum, a0, a1, a2, a3, qb[p][t][0], qb[p][t][1]);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) S[e] = p == C::Q_PARTS - 1 && t0 == 0 ? sum[e] : S[e] + sum[e];
+                for (int e = 0; e < 4; ++e) S[e] = p == C::Q_PARTS - 1 && t0 == 0 ? sum[e] : p == 0 && t0 == 0 ? fmaf(S[e], 1.f / PART, sum[e]) : S[e] + sum[e];
             }
     };
     // Weights of N x 16 keys, of which `rows` are there, from their logits, against the reference m (fac > 0); as B fragments.

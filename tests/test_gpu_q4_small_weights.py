@@ -1,5 +1,5 @@
-"""Small weights in attention over the 4-bit paged cache: a key that takes all the weight and has a value of zero, before thousands whose weights are
-e^-8 to e^-18 of it and make the output."""
+"""Small weights and small query channels in attention over the 4-bit paged cache: a key that takes all the weight and has a value of zero, before
+thousands whose weights are e^-8 to e^-18 of it and make the output; a query channel 2^-26 of the largest whose keys make the logits."""
 import numpy as np
 import pytest
 import torch
@@ -55,5 +55,32 @@ def test_a_sink_without_a_value(dtype, out_dtype, d, g, gap):
     o = (p * rv[1:].sum(0) / (1 + (n - 1) * p))[None, None]
     exact = F32 in (dtype, out_dtype)
     tol = (gap * 2.0 ** -23 * 2 + 2.0 ** -20 + (2.0 ** -20 if exact else 2.0 ** -10) + 2.0 ** -20 + 2 * _steps(n, exact) + (2.0 ** -24 if out_dtype == F32 else 2.0 ** -8)) * o
+    err = np.abs(out - o)
+    assert np.all(err <= tol), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("d,g", [(128, 4), (64, 3)])
+def test_a_small_query_channel(dtype, out_dtype, d, g):
+    """Channel 0 of a query is 2^26 times channel 1, and its keys are zero there: the logits come from channel 1, whose parts keep their bits (fp32: 22, bf16: all 8)."""
+    n = 130
+    rng = np.random.default_rng(3)
+    rk, rv = np.zeros((n, d)), rng.choice([0.5, 1.0, 1.5, 2.0, 3.0], (n, d))
+    rk[:, 1], rk[:, 2] = rng.choice([-6.0, -4.0, -3.0, -1.0, 1.0, 2.0, 4.0, 6.0], n) * 8192.0, 6 * 8192.0
+    rv[:, ::16] = 3.0
+    q = np.zeros((g, d))
+    q[:, 0] = 1.25
+    small = (1 + rng.integers(0, 1 << 23, g) / 2.0 ** 23) * 2.0 ** -26
+    q[:, 1] = torch.from_numpy(small).to(dtype).double().numpy()
+    scale = float(np.float32(8.0 / (6 * 8192 * 2.0 ** -26)))        # logits of 8 to 16
+    sh, qt, c, W = _shared(2, g, d, dtype, rk, rv, q, scale)
+    out = plain.decode(sh, qt, c, W, out_dtype).double().cpu().numpy()
+    s = q[:, 1:2] * rk[:, 1][None] * scale
+    p = np.exp(s - s.max(-1, keepdims=True))
+    p /= p.sum(-1, keepdims=True)
+    o, size = p @ rv, np.abs(s).max(-1, keepdims=True)
+    exact = F32 in (dtype, out_dtype)
+    # a logit's relative error: 2^-21 where a query is in two parts, 2^-22 from the factor and the product; it counts twice
+    tol = (2 * size * 2.0 ** -20 + 2.0 ** -20 + (2.0 ** -20 if exact else 2.0 ** -10) + 2.0 ** -20 + 2 * _steps(n, exact) + (2.0 ** -24 if out_dtype == F32 else 2.0 ** -8)) * o
     err = np.abs(out - o)
     assert np.all(err <= tol), float((err / tol).max())
