@@ -423,8 +423,10 @@ VECTOR_API size_t vector_decode_q4_workspace_bytes(const vector_shape* shape);
  * follows them.  A sequence with no rows gives zeros; an entry of a table outside its pool stands for rows that are not there.  A NaN in a key makes
  * its unit's outputs NaN, one in a value those of its 16 channels, and a NaN or an infinity among a head's queries that head's.
  * Arithmetic: products of stored rows are exact, sums fp32.  The softmax weights enter their products in fp16 (eleven bits, fewer under 2^-27 of the largest of
- * those summed up together, none under 2^-38; the sum of the weights is of the same rounded numbers), a key turned back (rope) too; with fp32 queries or fp32 output in
- * two fp16 parts each (22 bits), and fp32 queries in two; queries keep their bits down to 2^-28 of a head's largest channel.  The key sums, and an fp32 map, keep 24 bits on their way through the map.
+ * those summed up together, none under 2^-38; the sum of the weights is of the same rounded numbers), a key turned back (rope) too, by a sine, a cosine and products of
+ * eleven bits (of numbers under 2^-13, what is above 2^-24), and sums over rows are cut off to 24 bits, not rounded, after every 16 rows.  With fp32 queries or fp32 output: weights
+ * and turned keys in two fp16 parts each (22 bits), sums rounded.  fp32 queries enter in two parts; queries keep their bits down to 2^-28 of a head's largest channel.
+ * The key sums, and an fp32 map, keep 24 bits on their way through the map.
  * ws: at least vector_decode_q4_workspace_bytes() at a multiple of 256 bytes; calls that overlap on the GPU need workspaces of their own.
  * q: device [U][g][d] of shape->dtype; W: device [L * Hkv][d][d]; out: device [U][g][d] of out_dtype.
  */

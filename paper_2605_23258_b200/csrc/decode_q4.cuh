@@ -466,7 +466,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 }
             }
     };
-    // Sums of 16 rows x, times their weights; lo: second parts of the rows, where there are any.
+    // Sums of 16 rows x, times their weights; lo: second parts of the rows, where there are any, PART times as large.
     auto add_rows = [&](const uint32_t (&x)[2][C::PAIRS], const uint32_t (&ph)[2], const uint32_t (&pl)[2], const auto& lo, auto with_lo) {
 #pragma unroll
         for (int t = 0; t < C::O_TILES; ++t) {
@@ -474,13 +474,17 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             if constexpr (EXACT) {
                 float sum[4];
                 mma_alone(sum, a0, a1, a2, a3, ph[0], ph[1]);
-                if constexpr (!FOLD) {
+                if constexpr (!FOLD || with_lo.value) {
                     float second[4];
-                    mma_alone(second, a0, a1, a2, a3, pl[0], pl[1]);
+                    if constexpr (!FOLD) mma_alone(second, a0, a1, a2, a3, pl[0], pl[1]);
+                    if constexpr (with_lo.value) {
+                        const uint32_t l0 = transpose(lo[0][2 * t]), l1 = transpose(lo[0][2 * t + 1]), l2 = transpose(lo[1][2 * t]), l3 = transpose(lo[1][2 * t + 1]);
+                        if constexpr (FOLD) mma_alone(second, l0, l1, l2, l3, ph[0], ph[1]);
+                        else mma(second, l0, l1, l2, l3, ph[0], ph[1]);
+                    }
 #pragma unroll
                     for (int e = 0; e < 4; ++e) sum[e] = fmaf(second[e], 1.f / PART, sum[e]);
                 }
-                if constexpr (with_lo.value) mma(sum, transpose(lo[0][2 * t]), transpose(lo[0][2 * t + 1]), transpose(lo[1][2 * t]), transpose(lo[1][2 * t + 1]), ph[0], ph[1]);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) O[t][e] += sum[e];
             } else {
@@ -523,7 +527,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                         tc::unpack2(z, a, b);
                         hi = pack_h2(a, b);
                         const float2 f = unpack_h2(hi);
-                        low = pack_h2(a - f.x, b - f.y);
+                        low = pack_h2((a - f.x) * PART, (b - f.y) * PART);
                     };
                     parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
                     parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);

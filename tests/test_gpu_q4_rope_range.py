@@ -45,3 +45,16 @@ def test_far_positions(dtype, out_dtype, d, g, top):
     sh, q, c, W = plain.problem(2, 1, 1, g, d, dtype, [(0, 200), (90, 65)], 32, rope=True)
     c.apx_pos.copy_(torch.randint(top // 2, top, c.apx_pos.shape, generator=torch.Generator().manual_seed(1), dtype=torch.int32))
     plain.check_decode(sh, q, c, W, plain.decode(sh, q, c, W, out_dtype), True)
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, F32), (F32, F32)])
+@pytest.mark.parametrize("d,g,size", [(128, 4, 2.0 ** -7), (64, 4, 2.0 ** -12), (128, 8, 2.0 ** -12), (64, 6, 2.0 ** -7)])
+def test_small_keys_keep_their_parts(dtype, out_dtype, d, g, size):
+    """Keys far below one under fp32 results: a turned one has 22 bits (the tolerance is relative to its size)."""
+    sh, q, c, W = plain.problem(2, 1, 1, g, d, dtype, [(0, 150), (0, 65)], 33, rope=True)
+    pool, table = c.apx_pages.cpu().numpy(), c.apx_table.cpu().numpy()
+    rng = np.random.default_rng(5)
+    for b, n in ((0, 150), (1, 65)):
+        plain.put_rows(pool, plain.slots_of(table[b], n), 0, 0, rng.standard_normal((n, d)) * size)
+    c.apx_pages.copy_(torch.from_numpy(pool))
+    plain.check_decode(sh, q, c, W, plain.decode(sh, q, c, W, out_dtype), True)
