@@ -381,8 +381,8 @@ VECTOR_API size_t vector_q4_tile_bytes(const vector_shape* shape);
  * new_lengths[b]: the rows that it has then; first_row[b]: those that it had; row_start[b]: the sum of the positive changes before b, so that row_start[batch]
  * is all added rows; slots[row_start[b] + i]: the slot of its i-th added row, -1 where it got no page for it; slots behind the last added row are -1.  new_n_free:
  * the pages that are left on the stack.  new_lengths may be lengths, and new_n_free may be n_free; no other two of the buffers may overlap.
- * All device int32: lengths, added, new_lengths, first_row [batch], row_start [batch + 1], table [batch][width], free_pages [cap_free], n_free and
- * new_n_free [1], slots [n_slots] (NULL if n_slots is 0; rows beyond n_slots have no slot written; row starts stop at 2^31 - 1).  A negative length counts as none, a length beyond the table
+ * All device int32: lengths, added, new_lengths, first_row [batch], row_start [batch + 1], table [batch][width], free_pages [cap_free] (NULL if
+ * cap_free is 0), n_free and new_n_free [1], slots [n_slots] (NULL if n_slots is 0; rows beyond n_slots have no slot written; row starts stop at 2^31 - 1).  A negative length counts as none, a length beyond the table
  * as a full one.  batch <= 65535, width * page_rows < 2^31.
  */
 VECTOR_API vector_status vector_block_tables(int32_t batch, const int32_t* lengths, const int32_t* added, int32_t page_rows,

@@ -312,7 +312,7 @@ extern "C" vector_status vector_block_tables(int32_t batch, const int32_t* lengt
                                              int32_t width, int32_t* free_pages, int32_t cap_free, const int32_t* n_free, int32_t* new_lengths,
                                              int32_t* new_n_free, int32_t* first_row, int32_t* row_start, int32_t* slots, int64_t n_slots,
                                              void* stream) {
-    if (!lengths || !added || !table || !free_pages || !n_free || !new_lengths || !new_n_free || !first_row || !row_start) return VECTOR_ERR_NULL;
+    if (!lengths || !added || !table || (cap_free > 0 && !free_pages) || !n_free || !new_lengths || !new_n_free || !first_row || !row_start) return VECTOR_ERR_NULL;
     if (n_slots > 0 && !slots) return VECTOR_ERR_NULL;
     if (batch < 1 || batch > 65535 || page_rows < 1 || width < 1 || cap_free < 0 || n_slots < 0 || n_slots > 0x7fffffffLL ||
         (int64_t)width * page_rows > 0x7fffffffLL)
