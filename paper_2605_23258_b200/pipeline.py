@@ -104,13 +104,14 @@ class PagedCache:
     grow by a generated token a step, and end, each with a length of its own.
 
     shape.batch is the number of places; all device work is asynchronous on the current stream, and `append` and `decode` read nothing back, so
-    that a captured step follows the requests' lengths. 
+    that a captured step follows the requests' lengths.  Pages are counted on the device: whether an admission found enough of them is an answer on the
+    device, too.
     """
 
     def __init__(self, shape: B.Shape, ret_pages: int, apx_pages: int, ret_rows: int, apx_rows: int, positions: bool = True, device="cuda"):
         """Pools of so many pages; places for at most ret_rows retained and apx_rows key-only rows of a request."""
         self.shape, self.device = shape, device
-        pages = lambda rows: max(-(-rows // B.VECTOR_PAGE_ROWS), 1)  # noqa: E731
+        pages = lambda rows: max(self._pages(rows), 1)  # noqa: E731
         self.cache = B.alloc_q4_cache(shape, ret_pages, apx_pages, pages(ret_rows), pages(apx_rows), positions, device)
         n = shape.batch
         ints = lambda *size: torch.zeros(*size, dtype=torch.int32, device=device)  # noqa: E731
@@ -120,33 +121,42 @@ class PagedCache:
         self.active, self.first_row, self.row_start, self.slots = ints(n), ints(n), ints(n + 1), ints(n)
         self.ws = torch.empty(B.vector_decode_q4_workspace_bytes(shape), dtype=torch.uint8, device=device)
 
+    @staticmethod
+    def _pages(rows: int) -> int:
+        return -(-rows // B.VECTOR_PAGE_ROWS)
+
     def _change(self, tier: str, added, slots=None):
         c = self.cache
         table, length, stack, left = ((c.ret_table, c.ret_len, self.ret_free, self.n_ret_free) if tier == "ret"
                                       else (c.apx_table, c.apx_len, self.apx_free, self.n_apx_free))
         B.vector_block_tables(length, added, B.VECTOR_PAGE_ROWS, table, stack, left, length, left, self.first_row, self.row_start, slots)
 
-    def admit(self, place: int, comp: Compressor, K, V):
-        """Takes the routed context of a Compressor of one sequence (its score and route have been called) to an empty place."""
+    def admit(self, place: int, comp: Compressor, K, V) -> torch.Tensor:
+        """Takes the routed context of a Compressor of one sequence (its score and route have been called) to an empty place.  Returns whether
+        it is there, one bool on the device: where either pool has too few free pages left, nothing is taken, and the place stays without rows."""
         sh, b = comp.shape, comp.budget
         if sh.batch != 1 or (sh.n_layers, sh.n_kv_heads, sh.head_dim, sh.dtype) != (self.shape.n_layers, self.shape.n_kv_heads, self.shape.head_dim, self.shape.dtype):
             raise ValueError("the compressor is for one sequence of the same layers and heads")
-        slots = {}
+        there = ((self.n_ret_free >= self._pages(b.n_ret)) & (self.n_apx_free >= self._pages(b.n_apx)))[0]
+        slots, added = {}, {}
         for tier, n in (("ret", b.n_ret), ("apx", b.n_apx)):
             slots[tier] = torch.empty(n, dtype=torch.int32, device=self.device)
-            added = torch.zeros(self.shape.batch, dtype=torch.int32, device=self.device)
-            added[place] = n
-            self._change(tier, added, slots[tier])
-        B.vector_compact_q4(sh, b, K, V, comp.ret_idx, comp.apx_idx, self.cache, slots["ret"], slots["apx"])
-        self.active[place] = 1
+            added[tier] = torch.zeros(self.shape.batch, dtype=torch.int32, device=self.device)
+            added[tier][place] = there * n
+        for tier in ("ret", "apx"):
+            self._change(tier, added[tier], slots[tier])
+        B.vector_compact_q4(comp.shape, b, K, V, comp.ret_idx, comp.apx_idx, self.cache, slots["ret"], slots["apx"])
+        self.active[place] = there
+        return there
 
     def end(self, *places: int):
         """Gives the pages of these places back."""
+        at = list(places)
         gone = torch.zeros(self.shape.batch, dtype=torch.int32, device=self.device)
-        gone[list(places)] = -2**31
+        gone[at] = -2**31
         for tier in ("ret", "apx"):
             self._change(tier, gone)
-        self.active[list(places)] = 0
+        self.active[at] = 0
 
     def append(self, k_new, v_new, pos):
         """A generated token of every active place: k_new, v_new [U][d], pos [batch] int32.  A request that finds no page left keeps its length."""
