@@ -105,7 +105,7 @@ class PagedCache:
 
     shape.batch is the number of places; all device work is asynchronous on the current stream, and `append` and `decode` read nothing back, so
     that a captured step follows the requests' lengths.  Pages are counted on the device: whether an admission found enough of them is an answer on the
-    device, too.
+    device, too.  A place is taken from `admit` on, whatever that answered, until `end`.
     """
 
     def __init__(self, shape: B.Shape, ret_pages: int, apx_pages: int, ret_rows: int, apx_rows: int, positions: bool = True, device="cuda"):
@@ -120,10 +120,14 @@ class PagedCache:
         self.n_ret_free, self.n_apx_free = ints(1).fill_(ret_pages), ints(1).fill_(apx_pages)
         self.active, self.first_row, self.row_start, self.slots = ints(n), ints(n), ints(n + 1), ints(n)
         self.ws = torch.empty(B.vector_decode_q4_workspace_bytes(shape), dtype=torch.uint8, device=device)
+        self._taken = set()
 
     @staticmethod
     def _pages(rows: int) -> int:
         return -(-rows // B.VECTOR_PAGE_ROWS)
+
+    def _place(self, place: int) -> int:
+        return range(self.shape.batch)[place]
 
     def _change(self, tier: str, added, slots=None):
         c = self.cache
@@ -131,12 +135,25 @@ class PagedCache:
                                       else (c.apx_table, c.apx_len, self.apx_free, self.n_apx_free))
         B.vector_block_tables(length, added, B.VECTOR_PAGE_ROWS, table, stack, left, length, left, self.first_row, self.row_start, slots)
 
-    def admit(self, place: int, comp: Compressor, K, V) -> torch.Tensor:
-        """Takes the routed context of a Compressor of one sequence (its score and route have been called) to an empty place.  Returns whether
-        it is there, one bool on the device: where either pool has too few free pages left, nothing is taken, and the place stays without rows."""
-        sh, b = comp.shape, comp.budget
-        if sh.batch != 1 or (sh.n_layers, sh.n_kv_heads, sh.head_dim, sh.dtype) != (self.shape.n_layers, self.shape.n_kv_heads, self.shape.head_dim, self.shape.dtype):
+    def _check_admission(self, place: int, comp: Compressor, K, V):
+        sh, b, mine, c = comp.shape, comp.budget, self.shape, self.cache
+        if sh.batch != 1 or any(getattr(sh, f) != getattr(mine, f) for f in ("n_layers", "n_kv_heads", "head_dim", "dtype")):
             raise ValueError("the compressor is for one sequence of the same layers and heads")
+        if place in self._taken:
+            raise ValueError(f"place {place} is taken")
+        for n, table, pages, kind in ((b.n_ret, c.ret_table, c.ret_pages, "retained"), (b.n_apx, c.apx_table, c.apx_pages, "key-only")):
+            if self._pages(n) > table.shape[1]:
+                raise ValueError(f"{n} {kind} rows, and a place is for {table.shape[1] * B.VECTOR_PAGE_ROWS}")
+            if self._pages(n) > pages.shape[0]:
+                raise ValueError(f"{n} {kind} rows, and the pool of pages holds {pages.shape[0] * B.VECTOR_PAGE_ROWS}")
+
+    def admit(self, place: int, comp: Compressor, K, V) -> torch.Tensor:
+        """Takes the routed context of a Compressor of one sequence (its score and route have been called) to a place that is not taken.  Returns whether
+        it is there, one bool on the device: where either pool has too few free pages left, nothing is taken, and the place stays without rows.  What the host knows is refused
+        before anything changes: a taken place, a context longer than a place or a pool."""
+        place = self._place(place)
+        self._check_admission(place, comp, K, V)
+        b = comp.budget
         there = ((self.n_ret_free >= self._pages(b.n_ret)) & (self.n_apx_free >= self._pages(b.n_apx)))[0]
         slots, added = {}, {}
         for tier, n in (("ret", b.n_ret), ("apx", b.n_apx)):
@@ -147,16 +164,18 @@ class PagedCache:
             self._change(tier, added[tier], slots[tier])
         B.vector_compact_q4(comp.shape, b, K, V, comp.ret_idx, comp.apx_idx, self.cache, slots["ret"], slots["apx"])
         self.active[place] = there
+        self._taken.add(place)
         return there
 
     def end(self, *places: int):
         """Gives the pages of these places back."""
-        at = list(places)
+        at = [self._place(p) for p in places]
         gone = torch.zeros(self.shape.batch, dtype=torch.int32, device=self.device)
         gone[at] = -2**31
         for tier in ("ret", "apx"):
             self._change(tier, gone)
         self.active[at] = 0
+        self._taken.difference_update(at)
 
     def append(self, k_new, v_new, pos):
         """A generated token of every active place: k_new, v_new [U][d], pos [batch] int32.  A request that finds no page left keeps its length."""

@@ -65,3 +65,47 @@ def test_too_few_pages_are_left(ret_pages, apx_pages):
     assert p.active.tolist() == [0, 0, 1] and p.decode(q, W, out)[4:].any()
     for pages, n in zip(_held(p), (2, 4)):
         assert len(set(pages)) == len(pages) == n
+
+
+def test_what_the_host_knows_is_refused():
+    """Before anything changes: contexts longer than a place or a pool, a taken place, none."""
+    p = PagedCache(_shape(2), 4, 8, 200, 300)
+    comp, K, V = _context(400, 200)
+    p.admit(0, comp, K, V)
+    before = _state(p)
+    wide, far = _context(700, 300, 20), _context(900, 400, 170)           # 280 retained rows; 230, and 340 key-only ones
+    assert wide[0].budget.n_ret == 280 and far[0].budget.n_ret == 230 and far[0].budget.n_apx == 340
+    for args, what in (((1, *wide), "retained"), ((1, *far), "key-only"), ((0, comp, K, V), "place")):
+        with pytest.raises(ValueError, match=what):
+            p.admit(*args)
+        assert _same(_state(p), before), what
+    for place in (2, -3):
+        with pytest.raises(IndexError):
+            p.admit(place, comp, K, V)
+        with pytest.raises(IndexError):
+            p.end(place)
+        assert _same(_state(p), before)
+    small = PagedCache(_shape(2), 1, 8, 200, 300)
+    with pytest.raises(ValueError, match="pool"):
+        small.admit(0, comp, K, V)
+    assert bool(p.admit(-1, comp, K, V)) and p.cache.ret_len.tolist() == [100, 100]
+    p.end(-1, 0)
+    assert p.free_pages() == (4, 8) and not p.active.any()
+    assert bool(p.admit(1, comp, K, V))
+
+
+@pytest.mark.parametrize("rope", [0, 1])
+def test_no_key_only_rows_and_no_pages_for_them(rope):
+    """A budget that approximates nothing, over a cache without key-only pages."""
+    p = PagedCache(_shape(2, rope_enabled=rope), 6, 0, 300, 0)
+    comp, K, V = _context(400, 130, 0, rope_enabled=rope)
+    assert comp.budget.n_apx == 0
+    assert bool(p.admit(1, comp, K, V))
+    q, W = torch.randn(4, 2, D, device=DEV).bfloat16(), torch.randn(2, D, D, device=DEV).bfloat16()
+    out = p.decode(q, W, torch.empty(4, 2, D, device=DEV))
+    assert torch.isfinite(out).all() and out[2:].any() and not out[:2].any()
+    with pytest.raises(ValueError, match="key-only|pool"):
+        p.admit(0, *_context(400, 200, rope_enabled=rope))
+    assert p.free_pages() == (3, 0)
+    p.end(0, 1)
+    assert p.free_pages() == (6, 0)
