@@ -110,6 +110,8 @@ class PagedCache:
 
     def __init__(self, shape: B.Shape, ret_pages: int, apx_pages: int, ret_rows: int, apx_rows: int, positions: bool = True, device="cuda"):
         """Pools of so many pages; places for at most ret_rows retained and apx_rows key-only rows of a request."""
+        if shape.rope_enabled and not positions:
+            raise ValueError("keys with rotary positions are turned back by their positions: positions must be kept")
         self.shape, self.device = shape, device
         pages = lambda rows: max(self._pages(rows), 1)  # noqa: E731
         self.cache = B.alloc_q4_cache(shape, ret_pages, apx_pages, pages(ret_rows), pages(apx_rows), positions, device)
@@ -137,8 +139,10 @@ class PagedCache:
 
     def _check_admission(self, place: int, comp: Compressor, K, V):
         sh, b, mine, c = comp.shape, comp.budget, self.shape, self.cache
-        if sh.batch != 1 or any(getattr(sh, f) != getattr(mine, f) for f in ("n_layers", "n_kv_heads", "head_dim", "dtype")):
+        if sh.batch != 1 or any(getattr(sh, f) != getattr(mine, f) for f in ("n_layers", "n_kv_heads", "n_q_heads", "head_dim", "dtype")):
             raise ValueError("the compressor is for one sequence of the same layers and heads")
+        if bool(sh.rope_enabled) != bool(mine.rope_enabled) or (mine.rope_enabled and sh.rope_theta != mine.rope_theta):
+            raise ValueError("the compressor's rotary positions are not the cache's")
         if place in self._taken:
             raise ValueError(f"place {place} is taken")
         for n, table, pages, kind in ((b.n_ret, c.ret_table, c.ret_pages, "retained"), (b.n_apx, c.apx_table, c.apx_pages, "key-only")):
@@ -146,11 +150,14 @@ class PagedCache:
                 raise ValueError(f"{n} {kind} rows, and a place is for {table.shape[1] * B.VECTOR_PAGE_ROWS}")
             if self._pages(n) > pages.shape[0]:
                 raise ValueError(f"{n} {kind} rows, and the pool of pages holds {pages.shape[0] * B.VECTOR_PAGE_ROWS}")
+        for t, name in ((K, "K"), (V, "V")):
+            if B._sized(t, sh.torch_dtype, sh.units * b.n_tokens * sh.head_dim, name) % 16:
+                raise ValueError(f"{name} must lie at a multiple of 16 bytes")
 
     def admit(self, place: int, comp: Compressor, K, V) -> torch.Tensor:
         """Takes the routed context of a Compressor of one sequence (its score and route have been called) to a place that is not taken.  Returns whether
         it is there, one bool on the device: where either pool has too few free pages left, nothing is taken, and the place stays without rows.  What the host knows is refused
-        before anything changes: a taken place, a context longer than a place or a pool."""
+        before anything changes: a taken place, a context longer than a place or a pool, another model's."""
         place = self._place(place)
         self._check_admission(place, comp, K, V)
         b = comp.budget

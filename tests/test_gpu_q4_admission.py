@@ -68,14 +68,17 @@ def test_too_few_pages_are_left(ret_pages, apx_pages):
 
 
 def test_what_the_host_knows_is_refused():
-    """Before anything changes: contexts longer than a place or a pool, a taken place, none."""
+    """Before anything changes: contexts longer than a place or a pool, a taken place, none, other models' compressors, rows that compaction refuses."""
     p = PagedCache(_shape(2), 4, 8, 200, 300)
     comp, K, V = _context(400, 200)
     p.admit(0, comp, K, V)
     before = _state(p)
     wide, far = _context(700, 300, 20), _context(900, 400, 170)           # 280 retained rows; 230, and 340 key-only ones
     assert wide[0].budget.n_ret == 280 and far[0].budget.n_ret == 230 and far[0].budget.n_apx == 340
-    for args, what in (((1, *wide), "retained"), ((1, *far), "key-only"), ((0, comp, K, V), "place")):
+    for args, what in (((1, *wide), "retained"), ((1, *far), "key-only"), ((0, comp, K, V), "place"), ((1, *_context(400, 200, n_q_heads=8)), "layers and heads"),
+                       ((1, *_context(400, 200, rope_enabled=1)), "rotary"), ((1, comp, K[:1], V), "K"), ((1, comp, K, V.float()), "V"), ((1, comp, K.cpu(), V), "K"),
+                       ((1, comp, K.transpose(0, 1), V), "K"), ((1, comp, torch.empty(K.numel() + 1, dtype=K.dtype, device=DEV)[1:].view(K.shape), V), "K"),
+                       ((1, _context(500, 240, 160 // 2 + 1)[0], K, V), "K")):
         with pytest.raises(ValueError, match=what):
             p.admit(*args)
         assert _same(_state(p), before), what
@@ -92,6 +95,15 @@ def test_what_the_host_knows_is_refused():
     p.end(-1, 0)
     assert p.free_pages() == (4, 8) and not p.active.any()
     assert bool(p.admit(1, comp, K, V))
+
+
+def test_rotary_bases_and_positions():
+    p = PagedCache(_shape(2, rope_enabled=1, rope_theta=5e5), 4, 8, 200, 300)
+    with pytest.raises(ValueError, match="rotary"):
+        p.admit(0, *_context(400, 200, rope_enabled=1, rope_theta=1e4))
+    assert bool(p.admit(0, *_context(400, 200, rope_enabled=1, rope_theta=5e5)))
+    with pytest.raises(ValueError, match="positions"):
+        PagedCache(_shape(2, rope_enabled=1), 4, 8, 200, 300, positions=False)
 
 
 @pytest.mark.parametrize("rope", [0, 1])
