@@ -45,10 +45,11 @@ struct Call {
     }
     // No more units than multiprocessors: a large block a unit, since a unit's records are many then (8 units of 39 records, attention in all: 15.8 us, by blocks of 256
     // threads 23.5).  More: small blocks, and as many sequences for a map that is fetched once as leave one round of blocks (2048 units of eight sequences and
-    // one tile: 25.1 us, a unit a block 26.7; of 28 tiles 132.0 and 132.3).
+    // one tile: 25.1 us, a unit a block 26.7; of 28 tiles 132.0 and 132.3; fp32 maps of 128 channels, 2048 units of 256 sequences and 140 rows: 63.2, dealt as if three of
+    // these blocks shared a multiprocessor 72.6).
     template <typename T, int D, int HP> vector_status merge_heads(int workers) const {
         if (dm.U <= sm_count()) return merge_by<T, D, HP, MERGE_MOST>(1, workers);
-        const int resident = (sizeof(T) == 2 ? 4 : 3) * sm_count(), rounds = (dm.U + resident - 1) / resident;
+        const int resident = merge_blocks<T, D, MERGE_THREADS>() * sm_count(), rounds = (dm.U + resident - 1) / resident;
         return merge_by<T, D, HP, MERGE_THREADS>(rounds < c.batch ? rounds : c.batch, workers);
     }
     template <typename T, int D> vector_status merge(int workers) const {

@@ -700,10 +700,18 @@ template <typename T, int D> struct MapTile {
     }
 };
 
+// A merge block's own shared memory beside the map, and how many blocks a multiprocessor holds: by registers four (bf16 maps) or three, by its 228 KB of shared memory, of which
+// the system takes one a block, two of fp32 maps of 128 channels (64 KB).
+template <int D> constexpr int merge_shared() { return 2 * 8 * (D + 4) * 4 + 3 * 8 * 4 + 2 * 8 * MERGE_CHUNK * 4 + MERGE_CHUNK * 2 * 8 * 8; }
+template <typename T, int D, int THREADS> constexpr int merge_blocks() {
+    constexpr int by_registers = THREADS == MERGE_MOST ? 1 : sizeof(T) == 2 ? 4 : 3, by_memory = 228 * 1024 / (MapTile<T, D>::BYTES + merge_shared<D>() + 1024);
+    return by_memory < by_registers ? by_memory : by_registers;
+}
+
 // The records of `seqs` sequences' units of one (layer, KV head) into their outputs: the map is fetched once for all of them.
 // HP: pairs of heads; workers: of the streaming kernel.
 template <typename T, int D, int HP, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == MERGE_MOST ? 1 : sizeof(T) == 2 ? 4 : 3)
+__global__ void __launch_bounds__(THREADS, (merge_blocks<T, D, THREADS>()))
 decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, int workers, const T* W, void* __restrict__ out, int out_bf16) {
     constexpr int NW = THREADS / 32, GROUPS = THREADS / MERGE_THREADS, ROWS_W = 16, heads = 2 * HP;
     // Four numbers of a tier's sums are a thread's, ROUNDS times at the most: rows `row` and `row` + 8 of O tile t, heads 2 hp and 2 hp + 1.
