@@ -43,10 +43,10 @@ struct Call {
                                               dm.g, seqs, workers, (const T*)W, out, out_dtype == VECTOR_BF16 ? 1 : 0));
         return VECTOR_OK;
     }
-    // No more units than multiprocessors: a large block a unit, since a unit's records are many then (8 units of 39 records, attention in all: 15.8 us, by blocks of 256
-    // threads 23.5).  More: small blocks, and as many sequences for a map that is fetched once as leave one round of blocks (2048 units of eight sequences and
-    // one tile: 25.1 us, a unit a block 26.7; of 28 tiles 132.0 and 132.3; fp32 maps of 128 channels, 2048 units of 256 sequences and 140 rows: 63.2, dealt as if three of
-    // these blocks shared a multiprocessor 72.6).
+    // No more units than multiprocessors: a large block a unit, few records or many (attention in all, us, large and small blocks: 8 units of 2 tiles 12.9 and 13.8, of 41 tiles
+    // 14.8 and 20.1, 2 units of 617 tiles 50 and 72, 144 units of 2 tiles 14.9 and 16.0, of 39 tiles 22.8 and 25.8; more: 160 units 19.3 and 16.1, 28.0 and 25.7).  More units: small blocks, and as many sequences for a map that
+    // is fetched once as leave one round of blocks (2048 units of eight sequences and one tile: 25.1 us, a unit a block 26.7; of 28 tiles 132.0 and 132.3; fp32 maps of 128 channels,
+    // 2048 units of 256 sequences, three to five tiles each: 63.2, dealt as if three of these blocks shared a multiprocessor 72.6).
     template <typename T, int D, int HP> vector_status merge_heads(int workers) const {
         if (dm.U <= sm_count()) return merge_by<T, D, HP, MERGE_MOST>(1, workers);
         const int resident = merge_blocks<T, D, MERGE_THREADS>() * sm_count(), rounds = (dm.U + resident - 1) / resident;

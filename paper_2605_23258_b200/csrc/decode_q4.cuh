@@ -102,10 +102,14 @@ template <typename T, int D, bool ROPE, bool EXACT, bool FOLD> struct Cfg {
     static constexpr float ROW_UNIT = ROPE ? .5f : 1.f;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
-    // Rows of a softmax step, in sixteens.  us by (retained, key-only): 640 units of 3300 and 6550 rows (2, 1) 181, (1, 1) 181, (2, 2) 187; 2048 units of 650 and 1120 rows
-    // 124, 125, 134; rotary keys, 128 units of 3000 and 6000 rows 65.6, 66.8, 71.9; 64 channels, fp32 results 44.0, 44.8, 42.1.
+    // Rows of a softmax step, in sixteens.  us by (retained, key-only), 128 units of 3000 and 6000 rows, four heads: 128 channels (2, 1) 44.4, (1, 1) 45.1, (2, 2) 46.1, fp32 results 47.4,
+    // 47.9, 49.8, rotary keys 70.8, 70.6, 80, with fp32 results, by the costs (2, 3), 150, 148, 207; 64 channels (2, 2) 32.8, (2, 1) 33.9, (1, 1) 34.1, fp32 results 34.8, 35.9, 36.7, rotary keys, which take
+    // (2, 1): 47.1 either way, 48.7.
     static constexpr int N_RET = 2, N_APX = D == 64 && !ROPE ? 2 : 1;
-    using Cost = std::conditional_t<ROPE, Costs<2, 3>, Costs<4, 3>>;
+    // What tiles of the tiers cost, (retained, key-only).  us for 128 units of 3000 and 6000 rows, four heads, 128 channels and 64: (4, 3) 44 and 33, (1, 1) 47 and 35, (2, 1) 48 and
+    // 34, (2, 3) 52 and 40; fp32 results 47 and 35, 50 and 37, 51 and 37, 55 and 42.  Rotary keys: (2, 3) 70.8 and 47.0, (1, 2) 70.3 and 52.6, (1, 1) 78 and 48, (4, 3) 81 and 49; fp32 results,
+    // turned in two parts: (1, 2) 140 and 76, (2, 3) 150 and 80, (1, 1) 171 and 88, (4, 3) 189 and 91.  fp32 queries and eight heads order them alike.
+    using Cost = std::conditional_t<!ROPE, Costs<4, 3>, std::conditional_t<EXACT, Costs<1, 2>, Costs<2, 3>>>;
 };
 
 // Not volatile, like the transposes: the compiler may move them past one another, so that one's operands are on their way during the next.
