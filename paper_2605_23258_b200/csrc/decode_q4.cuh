@@ -151,6 +151,15 @@ __device__ __forceinline__ uint32_t pack_h2(float lo, float hi) {
     asm("cvt.rn.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
+// Weights, cut off at 65504, which they pass only where logits are 2^23 and more and their last places, by which the reference is lower, are ones.  NaN stays.
+__device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// The reference for a largest logit, which is rounded: under LEAD below it by one or two of its last places, so that the logit itself, before its rounding, is never the lower
+// one.  From 2^28 on it could be by 16 and more, and no weight would be left.  An infinite one stays, and gives NaN.
+__device__ __forceinline__ float reference(float top) { return top * (top > 0.f ? 1.f - 0x1p-23f : 1.f + 0x1p-23f) - LEAD; }
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
 // A worker's way through the sequence of tiles, as runs: tiles of one tier of one unit.
@@ -447,7 +456,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             for (int h = 0; h < 2; ++h) {
 #pragma unroll
                 for (int o = 4; o < 32; o <<= 1) top[h] = fmaxf(top[h], __shfl_xor_sync(0xffffffffu, top[h], o));
-                const float now = fmaxf(m[h], top[h] - LEAD), f = m[h] == now ? 1.f : tc::ex2(m[h] - now);
+                const float now = fmaxf(m[h], reference(top[h])), f = m[h] == now ? 1.f : tc::ex2(m[h] - now);
                 m[h] = now;
 #pragma unroll
                 for (int t = 0; t < C::O_TILES; ++t) { O[t][h] *= f; O[t][2 + h] *= f; }
@@ -459,10 +468,10 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const float a = tc::ex2(fmaf(S[i][2 * h], fac[0], -m[0])), b = tc::ex2(fmaf(S[i][2 * h + 1], fac[1], -m[1]));
-                const uint32_t hi = pack_h2(a, b);
+                const uint32_t hi = pack_weights(a, b);
                 if constexpr (EXACT) {
                     const float2 f = unpack_h2(hi);
-                    const uint32_t low = pack_h2((a - f.x) * PART, (b - f.y) * PART);
+                    const uint32_t low = pack_weights((a - f.x) * PART, (b - f.y) * PART);
                     ph[i][h] = transpose(FOLD && tig >= 2 ? low : hi);
                     if constexpr (!FOLD) pl[i][h] = transpose(low);
                 } else {
