@@ -216,11 +216,13 @@ struct Entry { int unit, rows, kind, edge; };
 
 // Phases of two neighbouring channel pairs, turns a position: multiples of 2^-32, and what these leave, in radians.
 struct __align__(16) TwoPhases { uint32_t turns[2]; float rest[2]; };
-__device__ __forceinline__ void put_phase(TwoPhases* to, int channel, unsigned long long phase) {
-    const uint32_t turns = (uint32_t)((phase + 0x80000000ull) >> 32);
-    to[channel / 2].turns[channel % 2] = turns;
-    to[channel / 2].rest[channel % 2] = (float)(int32_t)(uint32_t)phase * 3.4061215800865545e-19f;      // 2 pi / 2^64
+__device__ __forceinline__ void put_phase(TwoPhases& to, int which, unsigned long long phase) {
+    to.turns[which] = (uint32_t)((phase + 0x80000000ull) >> 32);
+    to.rest[which] = (float)(int32_t)(uint32_t)phase * 3.4061215800865545e-19f;      // 2 pi / 2^64
 }
+// Where the pair of channels 2 j, 2 j + 1 of piece tig's lies: what the four lanes of a quad read together is 64 bytes in a row (in the channels' order they met in one bank:
+// 128 units 70.9 us in place of 70.3).
+__device__ __forceinline__ constexpr int phase_place(int tig, int j) { return 4 * j + tig; }
 // Sine and cosine of a position times a phase.  Of the product modulo a turn the upper 23 bits count (8e-7): they become a number in [1, 2) and that a multiple of 2 pi
 // about zero, without a conversion from integers, which would wait for the unit that the sine and the cosine keep busy.  The phase's rest, under 2^-33 of a turn a position,
 // comes on top: 1e-4 at position 131072, 0.8 at 2^30 (16 sequences of 3000 and 6000 rows in 8 heads: 70.4 us, without it 67; by an integer product in its place 72.6).
@@ -268,7 +270,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     if constexpr (ROPE) {
         if (threadIdx.x < D / 2) {
             if constexpr (EXACT) phase64[threadIdx.x] = rope_phase_words(phases.phase[threadIdx.x]);
-            else put_phase(phase32, threadIdx.x, phases.phase[threadIdx.x]);
+            else put_phase(phase32[phase_place(threadIdx.x / (D / 8), threadIdx.x % (D / 8) / 2)], threadIdx.x % 2, phases.phase[threadIdx.x]);
         }
     }
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
@@ -545,7 +547,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                     parts(tc::fma2(u2, cs, tc::mul2(v2, sn)), u, lo[h][j]);
                     parts(tc::fma2(u2, tc::mul2(sn, tc::pack2(-1.f, -1.f)), tc::mul2(v2, cs)), v, lo[h][C::PAIRS / 2 + j]);
                 } else {
-                    const TwoPhases two = phase32[ch / 2];
+                    const TwoPhases two = phase32[phase_place(tig, j)];
                     const float at = (float)pos[h];
                     float c0, s0, c1, s1;
                     turn_cos_sin((uint32_t)pos[h], at, two.turns[0], two.rest[0], c0, s0);
