@@ -402,7 +402,7 @@ VECTOR_API vector_status vector_compact_q4(const vector_shape* shape, const vect
 /*
  * vector_append into pages: the rows of one generated token of every sequence, k_new and v_new (device [U][d]), rounded to 4 bits, go to slot
  * slots[row_start[b]] of the retained pool (row_start, slots: as vector_block_tables wrote them; a sequence with no new row has none written), or to slots[b] where
- * row_start is NULL; pos[b] (device; may be NULL where ret_pos is) becomes the row's entry of ret_pos.  A slot outside the pool, or a place outside the
+ * row_start is NULL (a sequence that grew by more rows has the first written, the others hold what was there); pos[b] (device; may be NULL where ret_pos is) becomes the row's entry of ret_pos.  A slot outside the pool, or a place outside the
  * n_slots slots, skips the row.
  */
 VECTOR_API vector_status vector_append_q4(const vector_shape* shape, const vector_q4_cache* cache, const void* k_new, const void* v_new,

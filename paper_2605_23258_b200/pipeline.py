@@ -105,7 +105,8 @@ class PagedCache:
 
     shape.batch is the number of places; all device work is asynchronous on the current stream, and `append` and `decode` read nothing back, so
     that a captured step follows the requests' lengths.  Pages are counted on the device: whether an admission found enough of them is an answer on the
-    device, too.  A place is taken from `admit` on, whatever that answered, until `end`.
+    device, too.  A place is taken from `admit` on, whatever that answered, until `end`.  A step covers all layers of the shape; a model
+    whose layers follow one another keeps a PagedCache a layer.
     """
 
     def __init__(self, shape: B.Shape, ret_pages: int, apx_pages: int, ret_rows: int, apx_rows: int, positions: bool = True, device="cuda"):
