@@ -337,6 +337,21 @@ VECTOR_API vector_status vector_decode_attn_layer(const vector_shape* shape, con
                                                   size_t ws_bytes, void* stream);
 
 /*
+ * ---- From projections -----------------------------------------------------------------------------
+ * Queries, keys and values as a layer's projections leave them, a token's heads behind one another, into the rows of the calls of this library, a head's
+ * tokens behind one another; queries and keys normed a head at a time and turned by their positions in the same pass.  (The paper takes both as given.)
+ *   y = x / sqrt(mean(x^2) + eps) * weight,  then the pair of channels (c, c + d/2) turned by pos theta^(-2c/d);  in fp32, rounded once.
+ * q: device [B][L][n_tokens] rows of Hq * d elements, q_stride elements apart, so that they may be part of a wider row; k, v: the same with Hkv * d.  Any of the three may be NULL.
+ * q_weight, k_weight: device [L][d] of shape->dtype; NULL: no norm.  Turned where shape->rope_enabled.  pos: device [B][n_tokens], NULL: a token's own index.
+ * q_out: device [U][g][n_tokens - q_first][d], the queries of tokens q_first on (q_first = n_tokens - w: the window of vector_score; one token a sequence: the q of
+ * vector_decode_attn); k_out, v_out: device [U][n_tokens][d] (the context; one token a sequence: rows to append).  Outputs overlap no input.
+ * All at multiples of 16 bytes, strides too (else VECTOR_ERR_SHAPE).  Squares are fp32: channels of 2^60 and more are no numbers of a norm.
+ */
+VECTOR_API vector_status vector_norm_rope(const vector_shape* shape, int64_t n_tokens, const void* q, int64_t q_stride, const void* q_weight,
+                                          int64_t q_first, void* q_out, const void* k, int64_t k_stride, const void* k_weight, void* k_out,
+                                          const void* v, int64_t v_stride, void* v_out, const int32_t* pos, float eps, void* stream);
+
+/*
  * ---- The mixed cache in 4 bits and pages ----------------------------------------------------------
  * What a server holds that keeps many sequences: rows of the mixed cache in 4 bits, in pages that sequences of different lengths
  * take and give back.  (The paper has no counterpart; what is attended to is the same, with rows rounded.)
@@ -431,6 +446,65 @@ VECTOR_API size_t vector_decode_q4_workspace_bytes(const vector_shape* shape);
  * q: device [U][g][d] of shape->dtype; W: device [L * Hkv][d][d]; out: device [U][g][d] of out_dtype.
  */
 VECTOR_API vector_status vector_decode_attn_q4(const vector_shape* shape, const void* q, const vector_q4_cache* cache, const void* W,
+                                               void* out, int32_t out_dtype, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * ---- The mixed cache in 8 bits and pages ----------------------------------------------------------
+ * The paged cache where four bits are too few: 129 bytes a row of 128 channels.  (The paper has no counterpart.)
+ *
+ *  - A channel is held as an e4m3 number (sign, four exponent bits, three mantissa bits, largest 448) times 2^e; a block of VECTOR_Q8_PAGE_ROWS
+ *    rows of one (layer, KV head), its keys or its values, shares e: the smallest in [-32, 31] with 448 2^e >= max |x|.  A channel is the nearest such number,
+ *    ties to the even one; what is larger than 448 2^31 is cut off there, infinities too; a NaN stays one and does not count for the scale.
+ *  - A page is such a block, of every (layer, KV head).  Row r of a sequence lies in page table[b][r / 32] at row r % 32; a sequence's new rows go
+ *    where its table and length say, so that these calls take no slots.  Pools: ret_pages [n_ret_pages][L * Hkv][2][tile], apx_pages
+ *    [n_apx_pages][L * Hkv][tile], tile = vector_q8_tile_bytes(); ret_pos and apx_pos [pages][L * Hkv][32].  All at multiples of 16 bytes; what lies behind a
+ *    sequence's last row may be anything.  Tables as vector_block_tables makes them with page_rows = 32; fewer than 2^26 pages a pool.
+ *  - Rows, queries and maps of these calls lie at multiples of 16 bytes (else VECTOR_ERR_SHAPE); at most VECTOR_Q4_MAX_BATCH
+ *    sequences in a call of vector_decode_attn_q8.  A page that a call writes belongs to one sequence.
+ */
+#define VECTOR_Q8_PAGE_ROWS 32
+typedef vector_q4_cache vector_q8_cache;
+
+/* Bytes of a page's 32 rows of one (layer, KV head): 4128 for 128 channels, 2080 for 64; 0 for an unsupported shape. */
+VECTOR_API size_t vector_q8_tile_bytes(const vector_shape* shape);
+
+/*
+ * vector_compact into pages: rows ret_idx of K and V and rows apx_idx of K become rows 0, 1, ... of the sequence's tiers, as far as ret_len and apx_len reach, their
+ * token indices go to ret_pos and apx_pos where those are not NULL.  What a sequence holds behind the written rows of a page is lost (its scale is the written rows'); pages
+ * behind are left as they were.  A token index outside the context gives a row of zeros; a page outside the pool takes no rows.
+ */
+VECTOR_API vector_status vector_compact_q8(const vector_shape* shape, const vector_budget* budget, const void* K, const void* V,
+                                           const int32_t* ret_idx, const int32_t* apx_idx, const vector_q8_cache* cache, void* stream);
+
+/*
+ * New rows of every sequence's retained tier, from one generated token to a piece of a prompt, keys turned by their positions on the way.  ret_len[b] counts the new
+ * rows already: rows first_row[b] .. ret_len[b] - 1 (first_row and ret_len: as vector_block_tables wrote them), n_new at the most, are k_new[b][0], k_new[b][1], ...; a sequence
+ * with fewer has none of the others read.  k_new, v_new: device [batch][n_new] rows of L * Hkv * d elements, k_stride and v_stride elements apart, so that
+ * they may be part of a wider row.  pos: device [batch][n_new], the tokens' positions; they go to ret_pos where that is not NULL (pos may be NULL where neither needs it).
+ * rotate != 0 (needs shape->rope_enabled, else VECTOR_ERR_SHAPE): the pair of channels (c, c + d/2) is turned by pos theta^(-2c/d), in fp32, before it is rounded.
+ * A new row that the scale of its block does not hold makes the scale larger, and the rows that are there are rounded again; the first row of a block begins a new scale.
+ */
+VECTOR_API vector_status vector_append_q8(const vector_shape* shape, const vector_q8_cache* cache, const void* k_new, int64_t k_stride,
+                                          const void* v_new, int64_t v_stride, int64_t n_new, const int32_t* first_row, const int32_t* pos,
+                                          int32_t rotate, void* stream);
+
+/*
+ * Rows read back as the values that they stand for: the first n_ret rows of every sequence to ret_k and ret_v (device [U][n_ret][d] of shape->dtype), the first
+ * n_apx key-only rows to apx_k (device [U][n_apx][d]).  Rows that a sequence does not have, and rows of a page outside the pool, are zeros.
+ */
+VECTOR_API vector_status vector_read_q8(const vector_shape* shape, const vector_q8_cache* cache, int64_t n_ret, void* ret_k, void* ret_v,
+                                        int64_t n_apx, void* apx_k, void* stream);
+
+/* Bytes of device workspace that vector_decode_attn_q8 needs for this shape, whatever the lengths. */
+VECTOR_API size_t vector_decode_q8_workspace_bytes(const vector_shape* shape);
+
+/*
+ * vector_decode_attn_q4 over the 8-bit pages: the same arguments, lengths read on the device, the same answers where rows are missing, and the same arithmetic: products of
+ * stored rows are exact, sums fp32, weights and turned keys in fp16 (in two parts with fp32 queries or output).  The scale of a block's keys is a factor of its logits, that of its
+ * values (and of key-only keys) one of the sums, which hold for the scale of the block before and change to the next one's.  A NaN in a key makes its unit's outputs NaN, one in a
+ * value that channel's.
+ */
+VECTOR_API vector_status vector_decode_attn_q8(const vector_shape* shape, const void* q, const vector_q8_cache* cache, const void* W,
                                                void* out, int32_t out_dtype, void* ws, size_t ws_bytes, void* stream);
 
 /*

@@ -161,6 +161,14 @@ class Q4Cache:
                               self.ret_table.shape[1], self.apx_table.shape[1])
 
 
+VECTOR_Q8_PAGE_ROWS = 32
+
+
+@dataclass
+class Q8Cache(Q4Cache):
+    """Device buffers of the 8-bit paged cache: as those of the 4-bit one, with pages of 32 rows."""
+
+
 def library_path() -> str:
     return _LIB_PATH
 
@@ -221,6 +229,17 @@ def load_library() -> ctypes.CDLL:
     lib.vector_decode_q4_workspace_bytes.restype = SZ
     lib.vector_decode_q4_workspace_bytes.argtypes = [SP]
     lib.vector_decode_attn_q4.argtypes = [SP, P, CP, P, P, I32, P, SZ, P]
+    lib.vector_q8_tile_bytes.restype = SZ
+    lib.vector_q8_tile_bytes.argtypes = [SP]
+    lib.vector_compact_q8.argtypes = [SP, BP, P, P, P, P, CP, P]
+    lib.vector_append_q8.argtypes = [SP, CP, P, I64, P, I64, I64, P, P, I32, P]
+    lib.vector_read_q8.argtypes = [SP, CP, I64, P, P, I64, P, P]
+    lib.vector_decode_q8_workspace_bytes.restype = SZ
+    lib.vector_decode_q8_workspace_bytes.argtypes = [SP]
+    lib.vector_decode_attn_q8.argtypes = [SP, P, CP, P, P, I32, P, SZ, P]
+    lib.vector_norm_rope.argtypes = [SP, I64, P, I64, P, I64, P, P, I64, P, P, P, I64, P, P, ctypes.c_float, P]
+    for name in ("vector_compact_q8", "vector_append_q8", "vector_read_q8", "vector_decode_attn_q8", "vector_norm_rope"):
+        getattr(lib, name).restype = ctypes.c_int
     for name in ("vector_block_tables", "vector_compact_q4", "vector_append_q4", "vector_read_q4", "vector_decode_attn_q4"):
         getattr(lib, name).restype = ctypes.c_int
     lib.vector_sync_check.argtypes = [P]
@@ -603,16 +622,16 @@ def _sized(t, dtype, n: int, name: str):
     return p
 
 
-def _q4(shape: Shape, cache: Q4Cache, attends: bool = False) -> bytes:
+def _q4(shape: Shape, cache: Q4Cache, attends: bool = False, tile: int = 0, page_rows: int = VECTOR_PAGE_ROWS) -> bytes:
     """The cache's struct, its tensors checked; tables and lengths where the call reads them."""
-    tile, LH = vector_q4_tile_bytes(shape), shape.n_layers * shape.n_kv_heads
+    tile, LH = tile or vector_q4_tile_bytes(shape), shape.n_layers * shape.n_kv_heads
     for t, n, name in ((cache.ret_pages, 2 * tile, "ret_pages"), (cache.apx_pages, tile, "apx_pages")):
         _dev(t, torch.uint8, name)
         if t.dim() != 3 or tuple(t.shape[1:]) != (LH, n):
             raise ValueError(f"{name} must be [pages][{LH}][{n}], got {tuple(t.shape)}")
     for t, pages, name in ((cache.ret_pos, cache.ret_pages, "ret_pos"), (cache.apx_pos, cache.apx_pages, "apx_pos")):
         if t is not None:
-            _sized(t, torch.int32, pages.shape[0] * LH * VECTOR_PAGE_ROWS, name)
+            _sized(t, torch.int32, pages.shape[0] * LH * page_rows, name)
     if attends:
         for t, n, name in ((cache.ret_table, cache.ret_len, "ret"), (cache.apx_table, cache.apx_len, "apx")):
             _dev(t, torch.int32, name + "_table")
@@ -717,6 +736,138 @@ def vector_decode_attn_q4(shape: Shape, q, cache: Q4Cache, W, out, ws=None, stre
                                               _sized(W, shape.torch_dtype, shape.n_layers * shape.n_kv_heads * d * d, "W"), _sized(out, out.dtype, n, "out"),
                                               VECTOR_BF16 if out.dtype == torch.bfloat16 else VECTOR_F32, wp, wn, _stream(stream))
     _check(rc, "vector_decode_attn_q4")
+
+
+# ---- the mixed cache in 8 bits and pages
+def _q8(shape: Shape, cache: Q8Cache) -> bytes:
+    """The cache's struct, its tensors checked: all calls but attention of one tier read its table and lengths, so both are."""
+    return _q4(shape, cache, True, vector_q8_tile_bytes(shape), VECTOR_Q8_PAGE_ROWS)
+
+
+def _rows(t, dtype, rows: int, width: int, name: str):
+    """Pointer and distance, in elements, of rows of `width` neighbouring elements each: the last dimensions of a tensor make up a row, the others count rows that lie evenly."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a CUDA tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must have dtype {dtype}, got {t.dtype}")
+    if t.numel() != rows * width:
+        raise ValueError(f"{name} must be {rows} rows of {width} elements, got {tuple(t.shape)}")
+    if t.is_contiguous():
+        return t.data_ptr(), width
+    sizes = [(n, s) for n, s in zip(t.shape, t.stride()) if n != 1]
+    at, run = len(sizes), 1
+    while run < width:                                    # a row
+        at -= 1
+        if sizes[at][1] != run or width % (run * sizes[at][0]):
+            raise ValueError(f"{name}: the {width} elements of a row must lie behind one another, got strides {t.stride()}")
+        run *= sizes[at][0]
+    if at == 0:
+        return t.data_ptr(), width
+    step = sizes[at - 1][1]
+    for (_, outer), (n, inner) in zip(sizes[:at], sizes[1:at]):
+        if outer != n * inner:
+            raise ValueError(f"{name}: rows must lie evenly, got strides {t.stride()}")
+    return t.data_ptr(), step
+
+
+def vector_q8_tile_bytes(shape: Shape) -> int:
+    """Bytes of a page's 32 rows of one (layer, KV head)."""
+    return int(load_library().vector_q8_tile_bytes(shape._p()))
+
+
+def alloc_q8_cache(shape: Shape, ret_pages: int, apx_pages: int, ret_width: int, apx_width: int, positions: bool = True, device="cuda") -> Q8Cache:
+    """Pools of so many pages, and tables of so many pages a sequence; no sequence has any rows."""
+    tile, LH, B = vector_q8_tile_bytes(shape), shape.n_layers * shape.n_kv_heads, shape.batch
+    ints = lambda *size: torch.empty(*size, dtype=torch.int32, device=device)  # noqa: E731
+    return Q8Cache(torch.empty(ret_pages, LH, 2 * tile, dtype=torch.uint8, device=device), torch.empty(apx_pages, LH, tile, dtype=torch.uint8, device=device),
+                   ints(B, ret_width).fill_(-1), ints(B, apx_width).fill_(-1), ints(B).zero_(), ints(B).zero_(),
+                   ints(ret_pages, LH, VECTOR_Q8_PAGE_ROWS) if positions else None, ints(apx_pages, LH, VECTOR_Q8_PAGE_ROWS) if positions else None)
+
+
+def vector_compact_q8(shape: Shape, budget: Budget, K, V, ret_idx, apx_idx, cache: Q8Cache, stream=None):
+    """Rows ret_idx of K and V and rows apx_idx of K become the first rows of the sequences' tiers, as far as the cache's lengths reach."""
+    rc = (_marshal_module or _marshal()).compact_q8(shape, budget, K, V, ret_idx, apx_idx, cache, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_compact_q8")
+        return
+    U, d = shape.units, shape.head_dim
+    rc = load_library().vector_compact_q8(shape._p(), budget._p(), _sized(K, shape.torch_dtype, U * budget.n_tokens * d, "K"),
+                                          _sized(V, shape.torch_dtype, U * budget.n_tokens * d, "V"),
+                                          _sized(ret_idx, torch.int32, U * budget.n_ret, "ret_idx"), _sized(apx_idx, torch.int32, U * budget.n_apx, "apx_idx"),
+                                          _q8(shape, cache), _stream(stream))
+    _check(rc, "vector_compact_q8")
+
+
+def vector_append_q8(shape: Shape, cache: Q8Cache, k_new, v_new, first_row, pos=None, rotate: bool = False, stream=None):
+    """k_new, v_new [batch][n] rows of L * Hkv * d elements: rows first_row[b] .. cache.ret_len[b] - 1 of every sequence, keys turned by pos [batch][n] where `rotate`."""
+    rc = (_marshal_module or _marshal()).append_q8(shape, cache, k_new, v_new, first_row, pos, rotate, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_append_q8")
+        return
+    B, width = shape.batch, shape.n_layers * shape.n_kv_heads * shape.head_dim
+    n = k_new.numel() // (B * width)
+    (kp, ks), (vp, vs) = _rows(k_new, shape.torch_dtype, B * n, width, "k_new"), _rows(v_new, shape.torch_dtype, B * n, width, "v_new")
+    rc = load_library().vector_append_q8(shape._p(), _q8(shape, cache), kp, ks, vp, vs, n, _sized(first_row, torch.int32, B, "first_row"),
+                                         None if pos is None else _sized(pos, torch.int32, B * n, "pos"), int(rotate), _stream(stream))
+    _check(rc, "vector_append_q8")
+
+
+def vector_read_q8(shape: Shape, cache: Q8Cache, ret_k=None, ret_v=None, apx_k=None, stream=None):
+    """The first n rows of every sequence as values [U][n][d]: retained ones to ret_k and ret_v, key-only ones to apx_k."""
+    rc = (_marshal_module or _marshal()).read_q8(shape, cache, ret_k, ret_v, apx_k, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_read_q8")
+        return
+    each, dt = shape.units * shape.head_dim, shape.torch_dtype
+    n_ret, n_apx = (0 if t is None else t.numel() // each for t in (ret_k, apx_k))
+    rc = load_library().vector_read_q8(shape._p(), _q8(shape, cache), n_ret, _sized(ret_k, dt, each * n_ret, "ret_k"), _sized(ret_v, dt, each * n_ret, "ret_v"),
+                                       n_apx, _sized(apx_k, dt, each * n_apx, "apx_k"), _stream(stream))
+    _check(rc, "vector_read_q8")
+
+
+def vector_decode_q8_workspace_bytes(shape: Shape) -> int:
+    return int(load_library().vector_decode_q8_workspace_bytes(shape._p()))
+
+
+def vector_decode_attn_q8(shape: Shape, q, cache: Q8Cache, W, out, ws=None, stream=None):
+    rc = (_marshal_module or _marshal()).decode_attn_q8(shape, q, cache, W, out, ws, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_decode_attn_q8")
+        return
+    wp, wn = _ws(ws)
+    if out.dtype not in (torch.float32, torch.bfloat16):
+        raise ValueError("out must be fp32 or bf16")
+    n, d = shape.units * shape.group * shape.head_dim, shape.head_dim
+    rc = load_library().vector_decode_attn_q8(shape._p(), _sized(q, shape.torch_dtype, n, "q"), _q8(shape, cache),
+                                              _sized(W, shape.torch_dtype, shape.n_layers * shape.n_kv_heads * d * d, "W"), _sized(out, out.dtype, n, "out"),
+                                              VECTOR_BF16 if out.dtype == torch.bfloat16 else VECTOR_F32, wp, wn, _stream(stream))
+    _check(rc, "vector_decode_attn_q8")
+
+
+# ---- from projections
+def vector_norm_rope(shape: Shape, n_tokens: int, q=None, k=None, v=None, q_out=None, k_out=None, v_out=None, q_weight=None, k_weight=None, pos=None, q_first: int = 0,
+                     eps: float = 1e-6, stream=None):
+    """q, k, v: [B][L][n_tokens] rows of a token's heads, or parts of wider rows -> q_out [U][g][n_tokens - q_first][d], k_out and v_out [U][n_tokens][d], queries and
+    keys normed a head at a time where they have a weight [L][d], and turned by pos [B][n_tokens] (None: a token's own index) where the shape has rotary positions."""
+    rc = (_marshal_module or _marshal()).norm_rope(shape, n_tokens, q, k, v, q_out, k_out, v_out, q_weight, k_weight, pos, q_first, eps, _handle(stream))
+    if rc is not None:
+        if rc:
+            _check(rc, "vector_norm_rope")
+        return
+    d, dt, L, BL = shape.head_dim, shape.torch_dtype, shape.n_layers, shape.batch * shape.n_layers
+    if not 0 <= q_first <= n_tokens:
+        raise ValueError(f"q_first must lie in [0, {n_tokens}], got {q_first}")
+    part = {}
+    for name, t, out, heads, first in (("q", q, q_out, shape.n_q_heads, q_first), ("k", k, k_out, shape.n_kv_heads, 0), ("v", v, v_out, shape.n_kv_heads, 0)):
+        part[name] = (None, 0, None) if t is None else (*_rows(t, dt, BL * n_tokens, heads * d, name), _sized(out, dt, BL * heads * (n_tokens - first) * d, name + "_out"))
+    wq, wk = (None if w is None else _sized(w, dt, L * d, name) for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")))
+    rc = load_library().vector_norm_rope(shape._p(), n_tokens, part["q"][0], part["q"][1], wq, q_first, part["q"][2], part["k"][0], part["k"][1], wk, part["k"][2],
+                                         *part["v"], None if pos is None else _sized(pos, torch.int32, shape.batch * n_tokens, "pos"), eps, _stream(stream))
+    _check(rc, "vector_norm_rope")
 
 
 VECTOR_STATIC_SCRATCH_BYTES = 16 << 20

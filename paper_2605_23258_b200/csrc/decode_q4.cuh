@@ -1,6 +1,6 @@
-// The kernels of attention over the 4-bit paged cache (decode_q4.cu).
+// The kernels of attention over the paged caches, in 4 bits (decode_q4.cu) and in 8 (decode_q8.cu).
 //
-// Streaming kernel.  A tile is a page of one unit: 64 keys and their values, or 64 key-only keys.  The sequence of all units' tiles, each
+// Streaming kernel.  A tile is a page of one unit: 64 keys and their values, or 64 key-only keys (8 bits: 32).  The sequence of all units' tiles, each
 // weighted by what it costs, is cut into equal contiguous ranges, one per warp: a warp is a worker of its own, which copies its tiles into
 // its own ring of slots (cp.async.bulk, one mbarrier a slot) and never waits for another warp.  It keeps one running state for a
 // unit's tier and writes it as a partial record when it leaves that.  The lengths lie on the device, so every block sums up the
@@ -13,6 +13,8 @@
 //   O^T += V^T P^T channels down, heads across; both operands are the registers at hand after an 8 x 8 transpose (movmatrix), and so are the key sums
 //                  A^T += K^T P^T of key-only keys, from the very registers that gave the logits
 // The sum of the weights is one more row of that product, a row of ones, so that a weight's rounding to fp16 is in numerator and denominator alike.
+// 8 bits: a row as fp16 is without its block's scale, a power of two.  That of keys is a factor of the tile's logits; that of values and of key-only keys is a factor
+// of the sums, which are kept for the scale of the tile before and multiplied, exactly, where the next one's is another.
 // Stored rows are exact in fp16, so the products are; halves of them too.  Queries are scaled by a power of two a head to fp16's range; fp32 queries take two fp16 parts.
 // EXACT (fp32 queries or fp32 output): weights, and keys turned back, in two fp16 parts, and sums of 16 keys added up outside the tensor cores,
 // which cut their sums off instead of rounding them.
@@ -27,6 +29,7 @@
 #include "common.cuh"
 #include "internal.h"
 #include "q4.cuh"
+#include "q8.cuh"
 #include "rope.cuh"
 #include "tcgen05.cuh"
 #include "tma.cuh"
@@ -51,9 +54,20 @@ struct Cache {
     int64_t n_ret_pages, n_apx_pages;
     int32_t ret_width, apx_width, LH, batch;
 };
+// What a tile is: rows in 4 bits, whose scales are part of them, or in 8.
+struct Bits4 {
+    static constexpr int ROWS = q4::ROWS;
+    static constexpr bool SCALED = false;                              // a tile has a scale of its own
+    template <int D> static constexpr int TILE = q4::Row<D>::TILE;
+};
+struct Bits8 {
+    static constexpr int ROWS = q8::ROWS;
+    static constexpr bool SCALED = true;
+    template <int D> static constexpr int TILE = q8::Row<D>::TILE;
+};
 // Rows of a sequence in a tier: what its table can hold at the most.
-__device__ __forceinline__ int rows_of(const int32_t* len, int b, int width) { return width ? min(max(len[b], 0), width * q4::ROWS) : 0; }
-__device__ __forceinline__ int tiles_of(int rows) { return (rows + q4::ROWS - 1) / q4::ROWS; }
+template <class F> __device__ __forceinline__ int rows_of(const int32_t* len, int b, int width) { return width ? min(max(len[b], 0), width * F::ROWS) : 0; }
+template <class F> __device__ __forceinline__ int tiles_of(int rows) { return (rows + F::ROWS - 1) / F::ROWS; }
 
 // ---- workspace: the first and the last worker of every unit that has tiles, then the records
 __host__ __device__ inline size_t ends_bytes(int units) { return ((size_t)units * 8 + 255) & ~(size_t)255; }
@@ -90,17 +104,18 @@ template <typename Cost> __device__ __forceinline__ int tile_from(int64_t r, int
 }
 
 // FOLD: EXACT with at most four heads, whose first and second parts of weights are eight columns of one product.
-template <typename T, int D, bool ROPE, bool EXACT, bool FOLD> struct Cfg {
+template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> struct Cfg {
     static_assert(EXACT || !FOLD, "one part needs no folding");
     static constexpr int WARPS = EXACT && D == 128 && (!FOLD || ROPE || sizeof(T) == 4) ? 8 : 12;
-    static constexpr int ENTRIES = WARPS == 12 ? 3 : 4;                // of a warp's ring, a tile each
     static constexpr int THREADS = 32 * WARPS;
-    static constexpr int POS_AT = q4::Row<D>::TILE;                    // of a key-only tile's positions, within an entry
-    static constexpr int ENTRY_BYTES = q4::Row<D>::TILE + (ROPE ? 4 * q4::ROWS : 0);
+    static constexpr int POS_AT = F::template TILE<D>;                 // of a key-only tile's positions, within an entry
+    static constexpr int ENTRY_BYTES = F::template TILE<D> + (ROPE ? 4 * F::ROWS : 0);
+    static constexpr int ENTRIES = F::SCALED ? 204 * 1024 / (WARPS * ENTRY_BYTES) : WARPS == 12 ? 3 : 4;        // of a warp's ring, a tile each
     static constexpr int SMEM_BYTES = WARPS * ENTRIES * ENTRY_BYTES;   // and behind them the prefix sums
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
     // Rows that may be turned are taken halved: a pair of stored channels, 61440 each, turns to 86889 at the most, and half of that is within fp16's 65504.
-    static constexpr float ROW_UNIT = ROPE ? .5f : 1.f;
+    // In 8 bits a turned pair is at most 634.
+    static constexpr float ROW_UNIT = ROPE && !F::SCALED ? .5f : 1.f;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
     // Rows of a softmax step, in sixteens.  us by (retained, key-only), 128 units of 3000 and 6000 rows, four heads: 128 channels (2, 1) 44.4, (1, 1) 45.1, (2, 2) 46.1, fp32 results 47.4,
@@ -164,33 +179,33 @@ __device__ __forceinline__ float reference(float top) { return top * (top > 0.f 
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
 // A worker's way through the sequence of tiles, as runs: tiles of one tier of one unit.
-template <typename Cost> struct Runs {
+template <class F, typename Cost> struct Runs {
     int64_t left;                               // cost up to the end of the worker's range
     int b, lh, n_ret, n_apx;                    // sequence, (layer, KV head), rows
     int apx, p, count;                          // the run: tier, first tile of it, tiles
     __device__ __forceinline__ void enter(const Cache& c) {
-        n_ret = rows_of(c.ret_len, b, c.ret_width);
-        n_apx = rows_of(c.apx_len, b, c.apx_width);
+        n_ret = rows_of<F>(c.ret_len, b, c.ret_width);
+        n_apx = rows_of<F>(c.apx_len, b, c.apx_width);
     }
     // The run that begins with tile t of the present unit, or of the next one if there is none; no tiles at the end of the range.
     __device__ __forceinline__ void run(const Cache& c, const int64_t* prefix, int t) {
-        int nr = tiles_of(n_ret);
-        if (t >= nr + tiles_of(n_apx)) {
+        int nr = tiles_of<F>(n_ret);
+        if (t >= nr + tiles_of<F>(n_apx)) {
             t = 0;
             if (++lh == c.LH) {
                 lh = 0;
                 do ++b; while (b < c.batch && prefix[b + 1] == prefix[b]);
-                if (b < c.batch) { enter(c); nr = tiles_of(n_ret); }
+                if (b < c.batch) { enter(c); nr = tiles_of<F>(n_ret); }
             }
         }
         apx = t >= nr;
         p = apx ? t - nr : t;
         const int each = apx ? Cost::apx : Cost::ret;
         const int64_t in_range = apx ? (left + Cost::apx - 1) / Cost::apx : (left + Cost::ret - 1) / Cost::ret;
-        count = b < c.batch ? (int)max(min((int64_t)((apx ? tiles_of(n_apx) : nr) - p), in_range), (int64_t)0) : 0;
+        count = b < c.batch ? (int)max(min((int64_t)((apx ? tiles_of<F>(n_apx) : nr) - p), in_range), (int64_t)0) : 0;
         left -= (int64_t)count * each;
     }
-    __device__ __forceinline__ void next(const Cache& c, const int64_t* prefix) { run(c, prefix, p + count + (apx ? tiles_of(n_ret) : 0)); }
+    __device__ __forceinline__ void next(const Cache& c, const int64_t* prefix) { run(c, prefix, p + count + (apx ? tiles_of<F>(n_ret) : 0)); }
     // The first run of the costs [x, end).
     __device__ __forceinline__ void find(const Cache& c, const int64_t* prefix, int64_t x, int64_t end) {
         int lo = 0, hi = c.batch;               // the last b with prefix[b] <= x
@@ -201,8 +216,8 @@ template <typename Cost> struct Runs {
         }
         b = lo;
         enter(c);
-        const int nr = tiles_of(n_ret);
-        const int64_t unit = (int64_t)Cost::ret * nr + (int64_t)Cost::apx * tiles_of(n_apx);
+        const int nr = tiles_of<F>(n_ret);
+        const int64_t unit = (int64_t)Cost::ret * nr + (int64_t)Cost::apx * tiles_of<F>(n_apx);
         lh = (int)divide(x - prefix[b], unit);
         const int64_t r = x - prefix[b] - lh * unit;
         const int t = tile_from<Cost>(r, nr);
@@ -249,12 +264,12 @@ template <int N> __device__ __forceinline__ void load_run(const __nv_bfloat16* p
     }
 }
 
-template <typename T, int D, bool ROPE, bool EXACT, bool FOLD>
-__global__ void __launch_bounds__(Cfg<T, D, ROPE, EXACT, FOLD>::THREADS, 1)
+template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4>
+__global__ void __launch_bounds__(Cfg<T, D, ROPE, EXACT, FOLD, F>::THREADS, 1)
 decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* ws, int* fault, RopePhases phases) {
-    using C = Cfg<T, D, ROPE, EXACT, FOLD>;
+    using C = Cfg<T, D, ROPE, EXACT, FOLD, F>;
     using R = q4::Row<D>;
-    constexpr int WARPS = C::WARPS, ENTRIES = C::ENTRIES;
+    constexpr int WARPS = C::WARPS, ENTRIES = C::ENTRIES, ROWS = F::ROWS, TILE = F::template TILE<D>;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ __align__(8) uint64_t full[WARPS][ENTRIES];
     __shared__ Entry entries[WARPS][ENTRIES];
@@ -282,7 +297,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         const int b = b0 + threadIdx.x;
         int64_t x = 0;
         if (b < c.batch)
-            x = (int64_t)c.LH * ((int64_t)C::Cost::ret * tiles_of(rows_of(c.ret_len, b, c.ret_width)) + (int64_t)C::Cost::apx * tiles_of(rows_of(c.apx_len, b, c.apx_width)));
+            x = (int64_t)c.LH * ((int64_t)C::Cost::ret * tiles_of<F>(rows_of<F>(c.ret_len, b, c.ret_width)) + (int64_t)C::Cost::apx * tiles_of<F>(rows_of<F>(c.apx_len, b, c.apx_width)));
         int64_t s = x;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -311,7 +326,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     const uint64_t policy = tma::policy_evict_first();
 
     // ---- the producing side, ENTRIES ahead: `run` is where it is, `k` tiles of it are on their way, and lane l has the page of tile l of 32
-    Runs<typename C::Cost> run;
+    Runs<F, typename C::Cost> run;
     run.find(c, prefix, deal.begin(worker), deal.begin(worker + 1));
     int k = 0, page = -1, values = 0;
     auto issue = [&](int s) {
@@ -322,17 +337,17 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             const bool there = at >= 0 && at < (run.apx ? c.n_apx_pages : c.n_ret_pages);
             const int p = run.p + k;
             const size_t tile = (size_t)at * c.LH + run.lh;
-            entries[wid][s] = Entry{run.b * c.LH + run.lh, there ? min((run.apx ? run.n_apx : run.n_ret) - p * q4::ROWS, (int)q4::ROWS) : 0,
+            entries[wid][s] = Entry{run.b * c.LH + run.lh, there ? min((run.apx ? run.n_apx : run.n_ret) - p * ROWS, ROWS) : 0,
                                     run.apx ? KEY_ONLY : values ? VALUES : KEYS,
-                                    (p == 0 && (!run.apx || run.n_ret == 0) ? 1 : 0) | (run.apx ? (p + 1) * q4::ROWS >= run.n_apx : run.n_apx == 0 && (p + 1) * q4::ROWS >= run.n_ret ? 1 : 0) << 1};
+                                    (p == 0 && (!run.apx || run.n_ret == 0) ? 1 : 0) | (run.apx ? (p + 1) * ROWS >= run.n_apx : run.n_apx == 0 && (p + 1) * ROWS >= run.n_ret ? 1 : 0) << 1};
             uint64_t* bar = &full[wid][s];
             unsigned char* to = ring + s * C::ENTRY_BYTES;
             if (!there) {
                 tma::mbar_arrive(bar);
             } else {
-                tma::mbar_expect_tx(bar, R::TILE + (ROPE && run.apx ? 4 * q4::ROWS : 0));
-                tma::load_bulk_hint(to, run.apx ? c.apx + tile * R::TILE : c.ret + (2 * tile + values) * R::TILE, R::TILE, bar, policy);
-                if (ROPE && run.apx) tma::load_bulk_hint(to + C::POS_AT, c.apx_pos + tile * q4::ROWS, 4 * q4::ROWS, bar, policy);
+                tma::mbar_expect_tx(bar, TILE + (ROPE && run.apx ? 4 * ROWS : 0));
+                tma::load_bulk_hint(to, run.apx ? c.apx + tile * TILE : c.ret + (2 * tile + values) * TILE, TILE, bar, policy);
+                if (ROPE && run.apx) tma::load_bulk_hint(to + C::POS_AT, c.apx_pos + tile * ROWS, 4 * ROWS, bar, policy);
             }
         }
         if (!run.apx) values ^= 1;
@@ -349,6 +364,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
 
     // ---- the consuming side
     uint32_t qb[C::Q_PARTS][C::O_TILES][2];
+    int held = 0;                                                      // SCALED: the sums are those times 2^-held
     float fac[2] = {0.f, 0.f}, m[2] = {-INFINITY, -INFINITY}, O[C::O_TILES][4], L[4];
     auto clear = [&] {
         m[0] = m[1] = -INFINITY;
@@ -390,11 +406,23 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             }
         }
     };
-    // Rows row0 + gid and row0 + gid + 8 of a tile as A fragments, times ROW_UNIT (exact: nothing stored is below 2^-18).
+    // Rows row0 + gid and row0 + gid + 8 of a tile as A fragments, times ROW_UNIT (exact: nothing stored is below 2^-18); SCALED: without the tile's scale.
     auto load_rows = [&](const unsigned char* tile, int row0, uint32_t (&x)[2][C::PAIRS]) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int row = row0 + 8 * h + gid;
+            if constexpr (F::SCALED) {
+                constexpr int N = D / 64;                              // runs of 16 bytes
+#pragma unroll
+                for (int i = 0; i < N; ++i) {
+                    const uint4 v = *reinterpret_cast<const uint4*>(tile + row * D + (D == 128 ? ((i ^ row) & 1) * 64 : 0) + tig * 16);
+                    q8::decode_word(v.x, x[h][8 * i], x[h][8 * i + 1]);
+                    q8::decode_word(v.y, x[h][8 * i + 2], x[h][8 * i + 3]);
+                    q8::decode_word(v.z, x[h][8 * i + 4], x[h][8 * i + 5]);
+                    q8::decode_word(v.w, x[h][8 * i + 6], x[h][8 * i + 7]);
+                }
+                continue;
+            }
             uint32_t w[4];
             if constexpr (D == 128) {
                 const uint4 v = *reinterpret_cast<const uint4*>(tile + row * R::CODES + tig * 16);
@@ -436,9 +464,23 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 for (int e = 0; e < 4; ++e) S[e] = p == C::Q_PARTS - 1 && t0 == 0 ? sum[e] : p == 0 && t0 == 0 ? fmaf(S[e], 1.f / PART, sum[e]) : S[e] + sum[e];
             }
     };
-    // Weights of N x 16 keys, of which `rows` are there, from their logits, against the reference m (fac > 0); as B fragments.
-    auto weigh = [&](auto& S, int rows, auto& ph, auto& pl) {
+    // SCALED: the sums change to a tile's scale.  Exponents lie in [-32, 31] and the sums below 2^56: nothing overflows.
+    auto hold = [&](int e) {
+        if (e == held) return;
+        const float f = q8::power(held - e);
+        held = e;
+#pragma unroll
+        for (int t = 0; t < C::O_TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) O[t][i] *= f;
+    };
+    // Weights of N x 16 keys, of which `rows` are there, from their logits, times 2^e, against the reference m (fac > 0); as B fragments.
+    auto weigh = [&](auto& S, int rows, auto& ph, auto& pl, int e) {
         constexpr int N = sizeof(S) / sizeof(S[0]);
+        float by[2] = {fac[0], fac[1]};
+        if constexpr (F::SCALED)                                       // above zero and finite: a masked logit stays -inf, a logit of zero that
+#pragma unroll
+            for (int h = 0; h < 2; ++h) by[h] = fminf(fmaxf(by[h] * q8::power(e), 1.2e-38f), 3.4e38f);
         if (rows < 16 * N) {
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -452,7 +494,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             top[h] = fmaxf(S[0][h], S[0][2 + h]);
 #pragma unroll
             for (int i = 1; i < N; ++i) top[h] = fmaxf(top[h], fmaxf(S[i][h], S[i][2 + h]));
-            top[h] *= fac[h];
+            top[h] *= by[h];
         }
         if (__any_sync(0xffffffffu, top[0] > m[0] + (LEAD + SLACK) || top[1] > m[1] + (LEAD + SLACK))) {
 #pragma unroll
@@ -470,7 +512,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         for (int i = 0; i < N; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const float a = tc::ex2(fmaf(S[i][2 * h], fac[0], -m[0])), b = tc::ex2(fmaf(S[i][2 * h + 1], fac[1], -m[1]));
+                const float a = tc::ex2(fmaf(S[i][2 * h], by[0], -m[0])), b = tc::ex2(fmaf(S[i][2 * h + 1], by[1], -m[1]));
                 const uint32_t hi = pack_weights(a, b);
                 if constexpr (EXACT) {
                     const float2 f = unpack_h2(hi);
@@ -580,7 +622,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         float4* o = reinterpret_cast<float4*>(p + 2 * heads);
 #pragma unroll
         for (int t = 0; t < C::O_TILES; ++t) {
-            constexpr float back = 1.f / C::ROW_UNIT;
+            const float back = F::SCALED ? q8::power(held) : 1.f / C::ROW_UNIT;
             o[(t * (heads / 2) + tig) * 8 + gid] = make_float4(O[t][0] * back, O[t][1] * back, O[t][2] * back, O[t][3] * back);
         }
     };
@@ -606,9 +648,11 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         --ahead;
         if (run.count > 0) { issue(s); ++ahead; __syncwarp(); }
     };
-    // What lies behind the last row may be no number: scales of zero there.
+    // What lies behind the last row may be no number: scales, or rows, of zero there.
     auto blank = [&](unsigned char* tile, int rows) {
-        for (int i = rows * R::GROUPS + lane; i < q4::ROWS * R::GROUPS; i += 32) tile[R::SCALES_AT + i] = 0;
+        if constexpr (F::SCALED)
+            for (int i = rows * D / 16 + lane; i < ROWS * D / 16; i += 32) reinterpret_cast<uint4*>(tile)[i] = make_uint4(0, 0, 0, 0);
+        else for (int i = rows * R::GROUPS + lane; i < q4::ROWS * R::GROUPS; i += 32) tile[R::SCALES_AT + i] = 0;
         asm volatile("fence.proxy.async.shared::cta;\n" ::: "memory");
         __syncwarp();
     };
@@ -643,7 +687,13 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             if (!wait()) return;
             tile = ring + at * C::ENTRY_BYTES;
             constexpr int N = C::N_RET;
-            if (entry.rows < q4::ROWS) blank(tile, entry.rows);
+            if (entry.rows < ROWS) blank(tile, entry.rows);
+            int of_logits = 0;
+            if constexpr (F::SCALED)
+                if (entry.rows > 0) {
+                    of_logits = q8::exponent_of(keys, TILE - 32);
+                    hold(q8::exponent_of(tile, TILE - 32));
+                }
 #pragma unroll 1
             for (int row0 = 0; row0 < entry.rows; row0 += 16 * N) {
                 uint32_t x[2][C::PAIRS], ph[N][2], pl[N][2];
@@ -653,7 +703,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                     load_rows(keys, row0 + 16 * i, x);
                     logits(x, S[i]);
                 }
-                weigh(S, entry.rows - row0, ph, pl);
+                weigh(S, entry.rows - row0, ph, pl, of_logits);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     load_rows(tile, row0 + 16 * i, x);
@@ -663,7 +713,9 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
             release(of_keys);
         } else {
             constexpr int N = C::N_APX;
-            if (entry.rows < q4::ROWS) blank(tile, entry.rows);
+            if (entry.rows < ROWS) blank(tile, entry.rows);
+            if constexpr (F::SCALED)
+                if (entry.rows > 0) hold(q8::exponent_of(tile, TILE - 32));
 #pragma unroll 1
             for (int row0 = 0; row0 < entry.rows; row0 += 16 * N) {
                 uint32_t x[N][2][C::PAIRS], ph[N][2], pl[N][2], lo[ROPE && EXACT ? N : 1][ROPE && EXACT ? 2 : 1][ROPE && EXACT ? C::PAIRS : 1];
@@ -672,7 +724,7 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
                 for (int i = 0; i < N; ++i) load_rows(tile, row0 + 16 * i, x[i]);
 #pragma unroll
                 for (int i = 0; i < N; ++i) logits(x[i], S[i]);
-                weigh(S, entry.rows - row0, ph, pl);
+                weigh(S, entry.rows - row0, ph, pl, held);
 #pragma unroll
                 for (int i = 0; i < N; ++i) {
                     if constexpr (ROPE) turn_back(tile, row0 + 16 * i, x[i], lo[EXACT ? i : 0]);
@@ -726,7 +778,7 @@ template <typename T, int D, int THREADS> constexpr int merge_blocks() {
 
 // The records of `seqs` sequences' units of one (layer, KV head) into their outputs: the map is fetched once for all of them.
 // HP: pairs of heads; workers: of the streaming kernel.
-template <typename T, int D, int HP, int THREADS>
+template <typename T, int D, int HP, int THREADS, class F = Bits4>
 __global__ void __launch_bounds__(THREADS, (merge_blocks<T, D, THREADS>()))
 decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, int workers, const T* W, void* __restrict__ out, int out_bf16) {
     constexpr int NW = THREADS / 32, GROUPS = THREADS / MERGE_THREADS, ROWS_W = 16, heads = 2 * HP;
@@ -751,7 +803,7 @@ decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, int workers, 
     };
     for (int b = b0; b < min(b0 + seqs, c.batch); ++b) {
         const int u = b * c.LH + lh;
-        const int n_apx = rows_of(c.apx_len, b, c.apx_width), n_ret = rows_of(c.ret_len, b, c.ret_width);
+        const int n_apx = rows_of<F>(c.apx_len, b, c.apx_width), n_ret = rows_of<F>(c.ret_len, b, c.ret_width);
         const int2 ends = reinterpret_cast<const int2*>(ws)[u];
         const float* records = reinterpret_cast<const float*>(ws + ends_bytes(units));
         const size_t o = (size_t)u * g * D;

@@ -38,6 +38,8 @@ vector_status check_budget(const vector_budget* b, int window);
 
 // Checks the pools of a 4-bit cache (not its tables and lengths, which attention alone reads).
 vector_status check_q4_cache(const vector_q4_cache* c);
+// Checks the pools and the tables' widths of an 8-bit cache.
+vector_status check_q8_cache(const vector_q8_cache* c);
 
 void set_last_cuda_error(int e);
 // Adds one to the process-wide count of kernels launched by the library (vector_kernel_launches).

@@ -21,7 +21,8 @@ namespace {
 #define ENTRY_POINTS(X) \
     X(vector_score) X(vector_route) X(vector_route_layer) X(vector_compact) X(vector_compact_layer) X(vector_append) X(vector_decode_attn) \
         X(vector_decode_attn_layer) X(vector_decode_attn_static) X(vector_block_tables) X(vector_compact_q4) X(vector_append_q4) X(vector_read_q4) \
-        X(vector_decode_attn_q4) X(vector_q4_tile_bytes)
+        X(vector_decode_attn_q4) X(vector_q4_tile_bytes) X(vector_compact_q8) X(vector_append_q8) X(vector_read_q8) X(vector_decode_attn_q8) X(vector_q8_tile_bytes) \
+        X(vector_norm_rope)
 #define POINTER(name) decltype(&::name) p_##name = nullptr;
 ENTRY_POINTS(POINTER)
 
@@ -197,11 +198,38 @@ struct Reader {
         c.n_apx = field(o, N_APX);
         return c;
     }
-    // attends: with the tables and lengths, which attention alone reads.
-    vector_q4_cache q4_cache(PyObject* o, const vector_shape& s, bool attends) {
+    // Rows of `width` neighbouring elements: contiguous ones, or those of a tensor whose last dimension, or last two, make up a row of evenly lying ones.
+    struct Rows { void* p = nullptr; int64_t stride = 0; };
+    Rows rows(PyObject* o, at::ScalarType type, int64_t count, int64_t width) {
+        Rows r;
+        const at::Tensor* t = tensor(o);
+        if (!t || !need(t->is_cuda() && t->scalar_type() == type && width > 0 && t->numel() == count * width)) return r;
+        r.p = t->data_ptr();
+        r.stride = width;
+        if (t->is_contiguous()) return r;
+        int64_t run = 1;
+        int at = (int)t->dim();
+        while (run < width) {
+            --at;
+            if (t->size(at) == 1) continue;
+            if (!need(t->stride(at) == run && width % (run * t->size(at)) == 0)) return r;
+            run *= t->size(at);
+        }
+        int64_t next = 0;                               // the distance of the next dimension's steps, 0: not known yet
+        while (--at >= 0) {
+            if (t->size(at) == 1) continue;
+            if (next == 0) r.stride = t->stride(at);
+            else if (!need(t->stride(at) == next)) return r;
+            next = t->stride(at) * t->size(at);
+        }
+        return r;
+    }
+    vector_q4_cache q8_cache(PyObject* o, const vector_shape& s) { return q4_cache(o, s, true, p_vector_q8_tile_bytes, VECTOR_Q8_PAGE_ROWS); }
+    // attends: with the tables and lengths, which of the 4-bit cache's calls attention alone reads.
+    vector_q4_cache q4_cache(PyObject* o, const vector_shape& s, bool attends, size_t (*tile_bytes)(const vector_shape*) = p_vector_q4_tile_bytes, int page_rows = VECTOR_PAGE_ROWS) {
         vector_q4_cache c = {};
         if (!plain || !need(q4_cache_class.covers(o))) return c;
-        const int64_t LH = (int64_t)s.n_layers * s.n_kv_heads, tile = (int64_t)p_vector_q4_tile_bytes(&s);
+        const int64_t LH = (int64_t)s.n_layers * s.n_kv_heads, tile = (int64_t)tile_bytes(&s);
         auto pages = [&](Name n, int64_t bytes, int64_t* count) -> void* {
             const Ref r(attr(o, n));
             void* p = plain ? device(r.o, at::kByte) : nullptr;
@@ -215,7 +243,7 @@ struct Reader {
         c.apx_pages = pages(APX_PAGES, tile, &c.n_apx_pages);
         auto positions = [&](Name n, int64_t count) -> int32_t* {
             const Ref r(attr(o, n));
-            return plain ? optional_ints(r.o, count * LH * VECTOR_PAGE_ROWS) : nullptr;
+            return plain ? optional_ints(r.o, count * LH * page_rows) : nullptr;
         };
         c.ret_pos = positions(RET_POS, c.n_ret_pages);
         c.apx_pos = positions(APX_POS, c.n_apx_pages);
@@ -446,6 +474,83 @@ METHOD(decode_attn_q4) {                                // shape, q, cache, W, o
         return run(r, [&] { return p_vector_decode_attn_q4(&s, q, &c, W, out.p, out.type, w.p, w.n, st); });
     });
 }
+METHOD(compact_q8) {                                    // shape, budget, K, V, ret_idx, apx_idx, cache, stream
+    return plain(n, 8, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        const vector_budget b = r.budget(a[1]);
+        const int64_t U = units_of(s), rows = U * b.n_tokens * s.head_dim;
+        void *k = r.sized(a[2], type_of(s), rows), *v = r.sized(a[3], type_of(s), rows);
+        const int32_t *ri = r.ints(a[4], U * b.n_ret), *ai = r.ints(a[5], U * b.n_apx);
+        const vector_q8_cache c = r.q8_cache(a[6], s);
+        void* st = r.stream(a[7]);
+        return run(r, [&] { return p_vector_compact_q8(&s, &b, k, v, ri, ai, &c, st); });
+    });
+}
+METHOD(append_q8) {                                     // shape, cache, k_new, v_new, first_row, pos, rotate, stream
+    return plain(n, 8, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        const vector_q8_cache c = r.q8_cache(a[1], s);
+        const int64_t width = (int64_t)s.n_layers * s.n_kv_heads * s.head_dim, each = width * s.batch;
+        if (!r.need(each > 0 && width > 0 && PyBool_Check(a[6]))) return 0L;
+        const int64_t rows = r.numel(a[2]) / each;
+        const Reader::Rows k = r.rows(a[2], type_of(s), s.batch * rows, width), v = r.rows(a[3], type_of(s), s.batch * rows, width);
+        const int32_t *first = r.ints(a[4], s.batch), *pos = r.optional_ints(a[5], s.batch * rows);
+        const int32_t rotate = a[6] == Py_True;
+        void* st = r.stream(a[7]);
+        return run(r, [&] { return p_vector_append_q8(&s, &c, k.p, k.stride, v.p, v.stride, rows, first, pos, rotate, st); });
+    });
+}
+METHOD(read_q8) {                                       // shape, cache, ret_k, ret_v, apx_k, stream
+    return plain(n, 6, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        const vector_q8_cache c = r.q8_cache(a[1], s);
+        const int64_t each = units_of(s) * s.head_dim;
+        if (!r.need(each > 0)) return 0L;
+        const int64_t n_ret = r.numel(a[2]) / each, n_apx = r.numel(a[4]) / each;
+        void *rk = r.sized(a[2], type_of(s), n_ret * each), *rv = r.sized(a[3], type_of(s), n_ret * each), *ak = r.sized(a[4], type_of(s), n_apx * each);
+        void* st = r.stream(a[5]);
+        return run(r, [&] { return p_vector_read_q8(&s, &c, n_ret, rk, rv, n_apx, ak, st); });
+    });
+}
+METHOD(decode_attn_q8) {                                // shape, q, cache, W, out, ws, stream
+    return plain(n, 7, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        if (!r.need(s.n_kv_heads > 0)) return 0L;
+        const int64_t rows = units_of(s) * (s.n_q_heads / s.n_kv_heads) * s.head_dim;
+        void* q = r.sized(a[1], type_of(s), rows);
+        const vector_q8_cache c = r.q8_cache(a[2], s);
+        void* W = r.sized(a[3], type_of(s), (int64_t)s.n_layers * s.n_kv_heads * s.head_dim * s.head_dim);
+        const Out out = r.output(a[4]);
+        r.need(r.numel(a[4]) >= rows);
+        const Workspace w = r.workspace(a[5]);
+        void* st = r.stream(a[6]);
+        return run(r, [&] { return p_vector_decode_attn_q8(&s, q, &c, W, out.p, out.type, w.p, w.n, st); });
+    });
+}
+METHOD(norm_rope) {                                     // shape, n_tokens, q, k, v, q_out, k_out, v_out, q_weight, k_weight, pos, q_first, eps, stream
+    return plain(n, 14, [&](Reader& r) {
+        const vector_shape s = r.shape(a[0]);
+        const int64_t N = r.integer(a[1]), first = r.integer(a[11]), BL = (int64_t)s.batch * s.n_layers, d = s.head_dim;
+        if (!r.need(s.batch > 0 && s.n_layers > 0 && s.n_q_heads > 0 && s.n_kv_heads > 0 && d > 0 && N > 0 && N <= (1 << 30) && first >= 0 && first <= N && PyFloat_Check(a[12]))) return 0L;
+        const at::ScalarType type = type_of(s);
+        Reader::Rows in[3];
+        void* out[3] = {};
+        for (int i = 0; i < 3 && r.plain; ++i)
+            if (a[2 + i] != Py_None) {
+                const int64_t heads = i == 0 ? s.n_q_heads : s.n_kv_heads;
+                in[i] = r.rows(a[2 + i], type, BL * N, heads * d);
+                out[i] = r.sized(a[5 + i], type, BL * heads * (i == 0 ? N - first : N) * d);
+            }
+        void* weight[2];
+        for (int i = 0; i < 2; ++i) weight[i] = a[8 + i] == Py_None ? nullptr : r.sized(a[8 + i], type, s.n_layers * d);
+        const int32_t* pos = r.optional_ints(a[10], s.batch * N);
+        const float eps = (float)PyFloat_AsDouble(a[12]);
+        void* st = r.stream(a[13]);
+        return run(r, [&] {
+            return p_vector_norm_rope(&s, N, in[0].p, in[0].stride, weight[0], first, out[0], in[1].p, in[1].stride, weight[1], out[1], in[2].p, in[2].stride, out[2], pos, eps, st);
+        });
+    });
+}
 // The library's entry points, by the handle of the library that ctypes has loaded, and the classes of the structs.
 METHOD(bind) {
     if (n != 5 || !PyLong_Check(a[0]) || !PyType_Check(a[1]) || !PyType_Check(a[2]) || !PyType_Check(a[3]) || !PyType_Check(a[4])) {
@@ -465,7 +570,7 @@ METHOD(bind) {
 #define ROW(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ROW(bind), ROW(score), ROW(route), ROW(route_layer), ROW(compact), ROW(compact_layer), ROW(append), ROW(append_rows),
                          ROW(decode_attn), ROW(decode_attn_layer), ROW(decode_attn_static), ROW(block_tables), ROW(compact_q4), ROW(append_q4),
-                         ROW(read_q4), ROW(decode_attn_q4), {nullptr, nullptr, 0, nullptr}};
+                         ROW(read_q4), ROW(decode_attn_q4), ROW(compact_q8), ROW(append_q8), ROW(read_q8), ROW(decode_attn_q8), ROW(norm_rope), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
