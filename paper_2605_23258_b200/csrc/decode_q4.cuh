@@ -110,7 +110,7 @@ template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> 
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int POS_AT = F::template TILE<D>;                 // of a key-only tile's positions, within an entry
     static constexpr int ENTRY_BYTES = F::template TILE<D> + (ROPE ? 4 * F::ROWS : 0);
-    static constexpr int ENTRIES = F::SCALED ? 204 * 1024 / (WARPS * ENTRY_BYTES) : WARPS == 12 ? 3 : 4;        // of a warp's ring, a tile each
+    static constexpr int ENTRIES = WARPS == 12 ? 3 : 4;                // of a warp's ring, a tile each
     static constexpr int SMEM_BYTES = WARPS * ENTRIES * ENTRY_BYTES;   // and behind them the prefix sums
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
     // Rows that may be turned are taken halved: a pair of stored channels, 61440 each, turns to 86889 at the most, and half of that is within fp16's 65504.
@@ -121,7 +121,9 @@ template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> 
     // Rows of a softmax step, in sixteens.  us by (retained, key-only), 128 units of 3000 and 6000 rows, four heads: 128 channels (2, 1) 44.4, (1, 1) 45.1, (2, 2) 46.1, fp32 results 47.4,
     // 47.9, 49.8, rotary keys 70.8, 70.6, 80, with fp32 results, by the costs (2, 3), 150, 148, 207; 64 channels (2, 2) 32.8, (2, 1) 33.9, (1, 1) 34.1, fp32 results 34.8, 35.9, 36.7, rotary keys, which take
     // (2, 1): 47.1 either way, 48.7.
-    static constexpr int N_RET = 2, N_APX = D == 64 && !ROPE ? 2 : 1;
+    // 8 bits, by steps of one and two sixteens of key-only rows: 64 units of 3277 and 6552 rows, eight heads, fp32 results of up to four heads and 128 channels 77.6 and 71.0,
+    // bf16 results 54.1 and 57.5, rotary keys 81.0 and 95.7, 64 channels 48.4 and 48.6.
+    static constexpr int N_RET = 2, N_APX = (D == 64 || (F::SCALED && FOLD && sizeof(T) == 2)) && !ROPE ? 2 : 1;
     // What tiles of the tiers cost, (retained, key-only).  us for 128 units of 3000 and 6000 rows, four heads, 128 channels and 64: (4, 3) 44 and 33, (1, 1) 47 and 35, (2, 1) 48 and
     // 34, (2, 3) 52 and 40; fp32 results 47 and 35, 50 and 37, 51 and 37, 55 and 42.  Rotary keys: (2, 3) 70.8 and 47.0, (1, 2) 70.3 and 52.6, (1, 1) 78 and 48, (4, 3) 81 and 49; fp32 results,
     // turned in two parts: (1, 2) 140 and 76, (2, 3) 150 and 80, (1, 1) 171 and 88, (4, 3) 189 and 91.  fp32 queries and eight heads order them alike.
@@ -681,12 +683,12 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         }
         unsigned char* tile = ring + at * C::ENTRY_BYTES;
         if (!tier) {
+            constexpr int N = C::N_RET;
             const unsigned char* keys = tile;
             const int of_keys = at;
             if (++at == ENTRIES) { at = 0; phase ^= 1; }
             if (!wait()) return;
             tile = ring + at * C::ENTRY_BYTES;
-            constexpr int N = C::N_RET;
             if (entry.rows < ROWS) blank(tile, entry.rows);
             int of_logits = 0;
             if constexpr (F::SCALED)

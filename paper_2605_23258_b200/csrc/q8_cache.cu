@@ -57,8 +57,45 @@ template <int D> struct Place {
     }
 };
 
-// The largest magnitude of all threads' numbers, as bits; NaN does not count.
-template <int N, int E> __device__ __forceinline__ uint32_t largest(const float (&x)[N][E], uint32_t* shared) {
+// The largest magnitude of a thread's stored numbers, as the bits of an fp32 number; NaN does not count.  Magnitudes order like their bits, NaN above all: where one
+// comes out, the slow way is taken.
+template <int N> __device__ __forceinline__ uint32_t largest_of(const uint4 (&v)[N], __nv_bfloat16) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        const uint32_t w[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) asm("max.u16x2 %0, %0, %1;\n" : "+r"(most) : "r"(w[i] & 0x7fff7fffu));
+    }
+    most = max(most & 0xffff0000u, most << 16);
+    if (most > 0x7f800000u) {
+        most = 0;
+#pragma unroll
+        for (int p = 0; p < N; ++p) {
+            const uint32_t w[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t size = (i & 1 ? w[i / 2] : w[i / 2] << 16) & 0x7fff0000u;
+                most = max(most, size > 0x7f800000u ? 0u : size);
+            }
+        }
+    }
+    return most;
+}
+template <int N> __device__ __forceinline__ uint32_t largest_of(const uint4 (&v)[N], float) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        const uint32_t w[4] = {v[p].x, v[p].y, v[p].z, v[p].w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t size = w[i] & 0x7fffffffu;
+            most = max(most, size > 0x7f800000u ? 0u : size);
+        }
+    }
+    return most;
+}
+template <int N, int E> __device__ __forceinline__ uint32_t largest_of(const float (&x)[N][E]) {
     uint32_t most = 0;
 #pragma unroll
     for (int p = 0; p < N; ++p)
@@ -67,6 +104,10 @@ template <int N, int E> __device__ __forceinline__ uint32_t largest(const float 
             const uint32_t size = __float_as_uint(x[p][i]) & 0x7fffffffu;
             most = max(most, size > 0x7f800000u ? 0u : size);
         }
+    return most;
+}
+// The largest of all threads' numbers.
+__device__ __forceinline__ uint32_t largest(uint32_t most, uint32_t* shared) {
     most = __reduce_max_sync(0xffffffffu, most);
     if (threadIdx.x % 32 == 0) shared[threadIdx.x / 32] = most;
     __syncthreads();
@@ -76,7 +117,8 @@ template <int N, int E> __device__ __forceinline__ uint32_t largest(const float 
     return most;
 }
 
-// Blocks of a unit: [0, br) retained keys, [br, 2 br) values, then key-only rows.  grid: (blocks, LH, batch).
+// Blocks of a unit: [0, br) retained keys, [br, 2 br) values, then key-only rows.  grid: (blocks, LH, batch).  The rows are on their way as soon as their indices are there, beside the
+// table and the length.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS)
 compact_kernel(const T* K, const T* V, int64_t N, const int32_t* ret_idx, const int32_t* apx_idx, int n_ret, int n_apx, Pools pools) {
@@ -86,32 +128,38 @@ compact_kernel(const T* K, const T* V, int64_t N, const int32_t* ret_idx, const 
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     const int lh = blockIdx.y, b = blockIdx.z, u = b * pools.LH + lh;
     const int br = (n_ret + ROWS - 1) / ROWS, which = (int)blockIdx.x < br ? 0 : (int)blockIdx.x < 2 * br ? 1 : 2;
-    const int block = blockIdx.x - which * br, n = which < 2 ? n_ret : n_apx;
-    const Place<D> place(pools, b, lh, which, block);
-    if (!place.tile) return;
-    const int rows = min(min(n, place.rows) - block * ROWS, ROWS);        // rows behind the sequence's last are left as they were
-    if (rows <= 0) return;
+    const int block = blockIdx.x - which * br, n = which < 2 ? n_ret : n_apx, given = min(n - block * ROWS, ROWS);
     const int32_t* idx = (which < 2 ? ret_idx : apx_idx) + (size_t)u * n + block * ROWS;
-    const T* src = (which == 1 ? V : K) + (size_t)u * N * D;
     const int lane = threadIdx.x % L::LANES, row0 = threadIdx.x / L::LANES;
-    float x[L::PASSES][L::E];
+    const T* src = (which == 1 ? V : K) + (size_t)u * N * D + lane * L::E;
+    int tok[L::PASSES];
+    uint4 v[L::PASSES];
+#pragma unroll
+    for (int p = 0; p < L::PASSES; ++p) tok[p] = row0 + p * L::PER < given ? idx[row0 + p * L::PER] : -1;
+    const Place<D> place(pools, b, lh, which, block);
 #pragma unroll
     for (int p = 0; p < L::PASSES; ++p) {
-        const int r = row0 + p * L::PER;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (r < rows) {
-            const int tok = idx[r];
-            if ((unsigned long long)(long long)tok < (unsigned long long)N) v = *reinterpret_cast<const uint4*>(src + (size_t)tok * D + lane * L::E);
-            if (lane == 0 && place.pos) place.pos[r] = tok;
-        }
-        widen(v, x[p]);
+        v[p] = make_uint4(0, 0, 0, 0);
+        if ((unsigned long long)(long long)tok[p] < (unsigned long long)N) v[p] = *reinterpret_cast<const uint4*>(src + (size_t)tok[p] * D);
     }
-    const int e = exponent(largest(x, shared));
+    if (!place.tile) return;
+    const int rows = min(place.rows - block * ROWS, given);               // rows behind the sequence's last are left as they were
+    if (rows <= 0) return;
+    if (rows < given) {
+#pragma unroll
+        for (int p = 0; p < L::PASSES; ++p)
+            if (row0 + p * L::PER >= rows) v[p] = make_uint4(0, 0, 0, 0);
+    }
+    const int e = exponent(largest(largest_of(v, T()), shared));
     const float inv = power(-e);
 #pragma unroll
     for (int p = 0; p < L::PASSES; ++p) {
         const int r = row0 + p * L::PER;
-        if (r < rows) put_codes(place.tile + r * D + Row<D>::byte_of(r, lane * L::E), x[p], inv);
+        if (r >= rows) continue;
+        float x[L::E];
+        widen(v[p], x);
+        put_codes(place.tile + r * D + Row<D>::byte_of(r, lane * L::E), x, inv);
+        if (lane == 0 && place.pos) place.pos[r] = tok[p];
     }
     if (threadIdx.x == 0) place.tile[Row<D>::SCALE_AT] = (unsigned char)(e - LOW);
 }
@@ -122,6 +170,11 @@ __global__ void __launch_bounds__(THREADS)
 append_kernel(const T* k_new, int64_t k_stride, const T* v_new, int64_t v_stride, int n_new, const int32_t* first_row, const int32_t* pos, Pools pools, RopePhases phases) {
     using L = Deal<T, D>;
     __shared__ uint32_t shared[THREADS / 32];
+    __shared__ RopePhase phase[ROTATE ? D / 2 : 1];                       // a thread's index into a kernel's parameters would be served a lane at a time
+    if constexpr (ROTATE) {
+        if (threadIdx.x < D / 2) phase[threadIdx.x] = rope_phase_words(phases.phase[threadIdx.x]);
+        __syncthreads();
+    }
     asm volatile("griddepcontrol.wait;\n" ::: "memory");
     asm volatile("griddepcontrol.launch_dependents;\n" ::: "memory");
     const int lh = blockIdx.y, b = blockIdx.z, is_v = blockIdx.x & 1;
@@ -136,39 +189,47 @@ append_kernel(const T* k_new, int64_t k_stride, const T* v_new, int64_t v_stride
     const int64_t stride = is_v ? v_stride : k_stride;
     const int lane = threadIdx.x % L::LANES, row0 = threadIdx.x / L::LANES;
     const int had = lo > 0 ? exponent_of(place.tile, Row<D>::SCALE_AT) : LOW;
+    uint4 v[L::PASSES];
+    int32_t at[L::PASSES];
+#pragma unroll
+    for (int p = 0; p < L::PASSES; ++p) {
+        const int r = row0 + p * L::PER;
+        const bool there = r >= lo && r < hi;
+        v[p] = make_uint4(0, 0, 0, 0);
+        if (there) v[p] = *reinterpret_cast<const uint4*>(src + r * stride + lh * D + lane * L::E);
+        at[p] = pos && there && !is_v ? pos[from + r] : 0;
+    }
     float x[L::PASSES][L::E];
 #pragma unroll
     for (int p = 0; p < L::PASSES; ++p) {
         const int r = row0 + p * L::PER;
         const bool there = r >= lo && r < hi;
-        uint4 v = make_uint4(0, 0, 0, 0);
-        if (there) v = *reinterpret_cast<const uint4*>(src + r * stride + lh * D + lane * L::E);
-        widen(v, x[p]);
-        int32_t at = 0;
-        if (pos && there && !is_v) {
-            at = pos[from + r];
-            if (lane == 0 && place.pos) place.pos[r] = at;
-        }
+        widen(v[p], x[p]);
+        if (there && lane == 0 && place.pos) place.pos[r] = at[p];
         if constexpr (ROTATE)
-            if (!is_v) {                                                  // the partner of a channel is half a row away
+            if (!is_v && __any_sync(0xffffffffu, there)) {                // the partner of a channel is half a row away
                 const bool upper = lane >= L::LANES / 2;
-                const int c = (lane % (L::LANES / 2)) * L::E;
+                // two lanes half a row apart have the same angles: each computes half of them
+                const int c = lane % (L::LANES / 2) * L::E + (upper ? L::E / 2 : 0);
+                float y[L::E];
+                widen(make_uint4(__shfl_xor_sync(0xffffffffu, v[p].x, L::LANES / 2), __shfl_xor_sync(0xffffffffu, v[p].y, L::LANES / 2),
+                                 __shfl_xor_sync(0xffffffffu, v[p].z, L::LANES / 2), __shfl_xor_sync(0xffffffffu, v[p].w, L::LANES / 2)), y);
 #pragma unroll
-                for (int i = 0; i < L::E; i += 2) {
-                    uint64_t cs2, sn2;
-                    rope_cos_sin2(rope_angle(at, rope_phase_words(phases.phase[c + i])), rope_angle(at, rope_phase_words(phases.phase[c + i + 1])), cs2, sn2);
-                    float cs[2], sn[2];
-                    tc::unpack2(cs2, cs[0], cs[1]);
-                    tc::unpack2(sn2, sn[0], sn[1]);
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        const float mine = x[p][i + j], other = __shfl_xor_sync(0xffffffffu, mine, L::LANES / 2);
-                        x[p][i + j] = fmaf(mine, cs[j], upper ? other * sn[j] : -other * sn[j]);
-                    }
+                for (int i = 0; i < L::E / 4; ++i) {
+                    uint64_t cs, sn;
+                    rope_cos_sin2_fine(rope_angle(at[p], phase[c + 2 * i]), rope_angle(at[p], phase[c + 2 * i + 1]), cs, sn);
+                    const uint64_t cs_o = __shfl_xor_sync(0xffffffffu, cs, L::LANES / 2), sn_o = __shfl_xor_sync(0xffffffffu, sn, L::LANES / 2);
+                    const uint64_t sign = upper ? 0ull : 0x8000000080000000ull;
+                    auto turn = [&](int k, uint64_t cs2, uint64_t sn2) {
+                        const uint64_t r = tc::fma2(tc::pack2(x[p][k], x[p][k + 1]), cs2, tc::mul2(tc::pack2(y[k], y[k + 1]), sn2 ^ sign));
+                        tc::unpack2(r, x[p][k], x[p][k + 1]);
+                    };
+                    turn(2 * i, upper ? cs_o : cs, upper ? sn_o : sn);
+                    turn(2 * i + L::E / 2, upper ? cs : cs_o, upper ? sn : sn_o);
                 }
             }
     }
-    const int e = max(exponent(largest(x, shared)), had);
+    const int e = max(exponent(largest(largest_of(x), shared)), had);
     if (e > had && lo > 0) {                                              // rows that were there, under the larger scale
         const float down = power(had - e);
         for (int i = threadIdx.x; i < lo * D / 4; i += THREADS) {
@@ -215,21 +276,25 @@ read_kernel(int n_ret, int n_apx, Pools pools, T* __restrict__ ret_k, T* __restr
     const int wanted = min(n - block * ROWS, ROWS), rows = place.tile ? min(place.rows - block * ROWS, wanted) : 0;
     const float s = rows > 0 ? power(exponent_of(place.tile, Row<D>::SCALE_AT)) : 0.f;
     T* out = (which == 0 ? ret_k : which == 1 ? ret_v : apx_k) + ((size_t)u * n + block * ROWS) * D;
+    constexpr int N = ROWS * RUNS / THREADS;                              // all of a thread's loads are on their way before the first store
+    uint2 w[N];
 #pragma unroll
-    for (int i = threadIdx.x; i < ROWS * RUNS; i += THREADS) {
-        const int r = i / RUNS, run = i % RUNS;
+    for (int p = 0; p < N; ++p) {
+        const int r = (p * THREADS + threadIdx.x) / RUNS, run = threadIdx.x % RUNS;
+        w[p] = make_uint2(0, 0);
+        if (r < rows) w[p] = *reinterpret_cast<const uint2*>(place.tile + r * D + Row<D>::byte_of(r, 8 * run));
+    }
+#pragma unroll
+    for (int p = 0; p < N; ++p) {
+        const int r = (p * THREADS + threadIdx.x) / RUNS, run = threadIdx.x % RUNS;
         if (r >= wanted) continue;
-        float x[8] = {};
-        if (r < rows) {
-            const uint2 w = *reinterpret_cast<const uint2*>(place.tile + r * D + Row<D>::byte_of(r, 8 * run));
-            float y[4];
-            decode_word(w.x, y);
+        float x[8], y[4];
+        decode_word(w[p].x, y);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = y[j] * s;
-            decode_word(w.y, y);
+        for (int j = 0; j < 4; ++j) x[j] = y[j] * s;
+        decode_word(w[p].y, y);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[4 + j] = y[j] * s;
-        }
+        for (int j = 0; j < 4; ++j) x[4 + j] = y[j] * s;
         put_run(out + (size_t)r * D + 8 * run, x);
     }
 }

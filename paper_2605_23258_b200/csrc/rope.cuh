@@ -22,6 +22,22 @@ __device__ __forceinline__ RopePhase rope_phase_words(unsigned long long phase) 
 __device__ __forceinline__ uint32_t rope_angle(int32_t pos, RopePhase ph) {
     return (uint32_t)pos * (uint32_t)ph.hi + (uint32_t)__mulhi(pos, ph.lo);
 }
+// Sines s and cosines c of what two angles are away from their nearest quarter turns, as those of the angles; u: an eighth of a turn more than the angles.
+__device__ __forceinline__ void rope_quarter_turns(uint32_t u0, uint32_t u1, uint64_t s, uint64_t c, uint64_t& cs2, uint64_t& sn2) {
+    float s0, s1, c0, c1;
+    tc::unpack2(s, s0, s1);
+    tc::unpack2(c, c0, c1);
+    auto turn = [](uint32_t u, float& cs, float& sn) {
+        const bool odd = (u & 0x40000000u) != 0;
+        const float a = odd ? sn : cs, b = odd ? cs : sn;
+        cs = __uint_as_float(__float_as_uint(a) ^ ((u + 0x40000000u) & 0x80000000u));
+        sn = __uint_as_float(__float_as_uint(b) ^ (u & 0x80000000u));
+    };
+    turn(u0, c0, s0);
+    turn(u1, c1, s1);
+    cs2 = tc::pack2(c0, c1);
+    sn2 = tc::pack2(s0, s1);
+}
 // Sine and cosine of two such angles.  Integer arithmetic takes an angle to the nearest quarter turn and
 // what remains of it, in [-pi/4, pi/4]; there the Taylor series about zero are good to 2e-9 (sine, five terms) and 2e-10 (cosine,
 // six), and a quarter turn swaps the two or changes their signs.
@@ -41,19 +57,30 @@ __device__ __forceinline__ void rope_cos_sin2(uint32_t angle0, uint32_t angle1, 
     s = tc::fma2(tc::mul2(s, zz), z, z);
     c = tc::fma2(c, zz, both(-0.5f));
     c = tc::fma2(c, zz, both(1.f));
-    float s0, s1, c0, c1;
-    tc::unpack2(s, s0, s1);
-    tc::unpack2(c, c0, c1);
-    auto turn = [](uint32_t u, float& cs, float& sn) {
-        const bool odd = (u & 0x40000000u) != 0;
-        const float a = odd ? sn : cs, b = odd ? cs : sn;
-        cs = __uint_as_float(__float_as_uint(a) ^ ((u + 0x40000000u) & 0x80000000u));
-        sn = __uint_as_float(__float_as_uint(b) ^ (u & 0x80000000u));
-    };
-    turn(u0, c0, s0);
-    turn(u1, c1, s1);
-    cs2 = tc::pack2(c0, c1);
-    sn2 = tc::pack2(s0, s1);
+    rope_quarter_turns(u0, u1, s, c, cs2, sn2);
+}
+// The same to less than a unit in the last place, for keys that are rounded to a few bits next: an error here moves numbers over the borders between them.  What remains of an angle is
+// kept in two parts, of its upper 24 bits (as a multiple of 256, exact) and the lower eight, and their product with 2 pi / 2^32 in two parts, too.
+__device__ __forceinline__ void rope_cos_sin2_fine(uint32_t angle0, uint32_t angle1, uint64_t& cs2, uint64_t& sn2) {
+    const uint32_t u0 = angle0 + 0x20000000u, u1 = angle1 + 0x20000000u;
+    auto both = [](float x) { return tc::pack2(x, x); };
+    auto high = [](uint32_t u) { return (float)((int)(u & 0x3fffff00u) - 0x20000000); };
+    auto low = [](uint32_t u) { return __uint_as_float(0x4b000000u | (u & 0xffu)) - 8388608.f; };
+    const uint64_t h = tc::pack2(high(u0), high(u1)), l = tc::pack2(low(u0), low(u1)), unit = both(1.4629180792671596e-9f);      // 2 pi / 2^32, and what that leaves of it
+    const uint64_t z = tc::mul2(h, unit);
+    const uint64_t rest = tc::fma2(l, unit, tc::fma2(h, both(-4.0709404e-17f), tc::fma2(h, unit, z ^ 0x8000000080000000ull)));
+    const uint64_t zz = tc::mul2(z, z);
+    uint64_t s = tc::fma2(both(1.f / 362880.f), zz, both(-1.f / 5040.f));
+    uint64_t c = tc::fma2(both(-1.f / 3628800.f), zz, both(1.f / 40320.f));
+    s = tc::fma2(s, zz, both(1.f / 120.f));
+    c = tc::fma2(c, zz, both(-1.f / 720.f));
+    s = tc::fma2(s, zz, both(-1.f / 6.f));
+    c = tc::fma2(c, zz, both(1.f / 24.f));
+    // sin(z + rest) = z + (z^3 s + rest cos z), cos(z + rest) = 1 + (z^2 (z^2 c - 1/2) - rest z)
+    s = tc::fma2(tc::mul2(s, zz), z, tc::fma2(tc::mul2(rest, both(-0.5f)), zz, rest));
+    c = tc::fma2(tc::fma2(c, zz, both(-0.5f)), zz, tc::mul2(rest, z) ^ 0x8000000080000000ull);
+    const uint64_t one = both(1.f);
+    rope_quarter_turns(u0, u1, tc::fma2(s, one, z), tc::fma2(c, one, one), cs2, sn2);
 }
 
 // A pair of numbers as bf16 parts, each a part of what the ones before it leave.  Three are the upper halves of the words, cut off:
