@@ -1,6 +1,5 @@
-// Generation-time attention over the 8-bit paged cache (q8.cuh).  128 channels without rotary positions: decode_q8_tc.cuh, where stored rows are operands of the tensor cores as they are.
-// Keys that are turned back, and 64 channels: the kernel of the 4-bit pages, in decode_q4.cuh, with another kind of tile.  The merge is the same for all.
-#include "decode_q8_tc.cuh"
+// Generation-time attention over the 8-bit paged cache (q8.cuh).  The kernels are those of the 4-bit pages, in decode_q4.cuh, with another kind of tile.
+#include "decode_q4.cuh"
 
 namespace vec {
 namespace dq8 {             // names of its own: the linker keeps one of two functions of the same name
@@ -32,29 +31,6 @@ struct Call {
                                               dm.scale * 1.4426950408889634f, ws, fault, ph));
         return merge<T, D>(sm_count() * C::WARPS);
     }
-    template <typename T, bool EXACT, int G> vector_status tensor_cores() const {
-        using C = TcCfg<T, EXACT, G>;
-        constexpr int tile = q8::Row<CHANNELS>::TILE;
-        static_assert(C::smem(MAX_BATCH) + 2048 <= 227 * 1024, "a block's shared memory, its own variables included");
-        auto kern = decode_q8_stream_tc<T, EXACT, G>;
-        static PerDeviceOnce once;
-        if (once.first()) {
-            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)C::smem(MAX_BATCH));
-            if (e != cudaSuccess) { once.undo(); VEC_CUDA_CHECK(e); }
-        }
-        int* fault = kernel_fault_address();
-        if (!fault) return VECTOR_ERR_CUDA;
-        TcMaps maps = {};
-        bool ok = true;
-        for (int half = 0; half < 2; ++half) {                            // a row's half lies 64 bytes on in odd rows if it is the first, back if it is the second
-            const uint64_t to_odd = half ? 64 : 192;
-            if (c.n_ret_pages > 0) ok = ok && tma::encode_u8_4d(&maps.ret[half], c.ret + 64 * half, 2, q8::ROWS / 2, (uint64_t)c.n_ret_pages * c.LH * 2, to_odd, 256, tile);
-            if (c.n_apx_pages > 0) ok = ok && tma::encode_u8_4d(&maps.apx[half], c.apx + 64 * half, 2, q8::ROWS / 2, (uint64_t)c.n_apx_pages * c.LH, to_odd, 256, tile);
-        }
-        if (!ok) return VECTOR_ERR_CUDA;
-        VEC_CUDA_CHECK(launch_maybe_dependent(true, kern, dim3(sm_count()), dim3(C::THREADS), C::smem(c.batch), st, maps, (const T*)q, c, dm.g, dm.scale * 1.4426950408889634f, ws, fault));
-        return merge<T, CHANNELS>(sm_count());
-    }
     template <typename T, int D, int HP, int THREADS> vector_status merge_by(int seqs, int workers) const {
         auto kern = decode_q4_merge<T, D, HP, THREADS, Bits8>;
         constexpr int smem = MapTile<T, D>::BYTES;
@@ -81,19 +57,10 @@ struct Call {
     }
     template <typename T, int D> vector_status run() const {
         const bool exact = dm.dtype == VECTOR_F32 || out_dtype == VECTOR_F32;
-        if constexpr (D == CHANNELS) {
-            if (dm.rope) return turned<T, D, true>(exact);
-            if constexpr (sizeof(T) == 2)
-                if (!exact) return dm.g <= 4 ? tensor_cores<T, false, 4>() : tensor_cores<T, false, 8>();
-            return dm.g <= 4 ? tensor_cores<T, true, 4>() : tensor_cores<T, true, 8>();
-        } else {
-            return dm.rope ? turned<T, D, true>(exact) : turned<T, D, false>(exact);
-        }
-    }
-    template <typename T, int D, bool ROPE> vector_status turned(bool exact) const {
         if constexpr (sizeof(T) == 2)
-            if (!exact) return both<T, D, ROPE, false, false>();
-        return dm.g <= 4 ? both<T, D, ROPE, true, true>() : both<T, D, ROPE, true, false>();
+            if (!exact) return dm.rope ? both<T, D, true, false, false>() : both<T, D, false, false, false>();
+        if (dm.g <= 4) return dm.rope ? both<T, D, true, true, true>() : both<T, D, false, true, true>();
+        return dm.rope ? both<T, D, true, true, false>() : both<T, D, false, true, false>();
     }
 };
 
@@ -122,8 +89,6 @@ extern "C" vector_status vector_decode_attn_q8(const vector_shape* shape, const 
     if (cache->ret_width > 0 && (!cache->ret_table || !cache->ret_len)) return VECTOR_ERR_NULL;
     if (cache->apx_width > 0 && (!cache->apx_table || !cache->apx_len)) return VECTOR_ERR_NULL;
     if (dm.rope && cache->n_apx_pages > 0 && !cache->apx_pos) return VECTOR_ERR_NULL;
-    // a tile's number is a coordinate of 32 bits; so many pages would be 8 TB
-    if (2 * cache->n_ret_pages * dm.LH > 0x7fffffffLL || cache->n_apx_pages * dm.LH > 0x7fffffffLL) return VECTOR_ERR_SHAPE;
     if (!ws || ((uintptr_t)ws & 255) || ws_bytes < dq8::ws_bytes_of(dm)) return VECTOR_ERR_WORKSPACE;
     if (((uintptr_t)q | (uintptr_t)W | (uintptr_t)out | (uintptr_t)cache->apx_pos) & 15) return VECTOR_ERR_SHAPE;
     const dq4::Cache c = {(const unsigned char*)cache->ret_pages, (const unsigned char*)cache->apx_pages, cache->ret_table, cache->apx_table,

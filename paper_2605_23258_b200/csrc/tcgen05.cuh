@@ -79,29 +79,6 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr) {
     d |= (uint64_t)2 << 61;                 // 128-byte swizzle
     return d;
 }
-// D[tmem] (+)= A[smem] B[smem]^T of 8-bit numbers, 32 of K, fp32 accumulation (the sum of 128 products of the whole range of e4m3: off by 2^-21.7 of the sum of their magnitudes at the most,
-// by nothing where the products lie within 2^16 of one another).
-__device__ __forceinline__ void mma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n}\n"
-        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate) : "memory");
-}
-// Shared-memory operand descriptors of bytes, by their swizzle; `group`: bytes between groups of eight rows (without a swizzle and with the rows contiguous in M or N: between runs of 16 of M or N),
-// `lead`: between blocks of M or N where these are contiguous (without a swizzle: between groups of eight rows of K); not used by rows contiguous in K.
-enum Swizzle : uint32_t { NONE = 0, BYTES128 = 2, BYTES64 = 4 };
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, Swizzle swizzle, uint32_t group, uint32_t lead = 16) {
-    uint64_t d = (uint64_t)((addr & 0x3FFFFu) >> 4);
-    d |= (uint64_t)(lead >> 4) << 16;
-    d |= (uint64_t)(group >> 4) << 32;
-    d |= (uint64_t)1 << 46;
-    d |= (uint64_t)swizzle << 61;
-    return d;
-}
-// Instruction descriptor: fp32 accumulator, e4m3 A and B; a_m, b_n: rows contiguous in M, N, not in K.
-__host__ __device__ constexpr uint32_t instr_desc_f8(int M, int N, bool a_m, bool b_n) {
-    return (1u << 4) | (a_m ? 1u << 15 : 0u) | (b_n ? 1u << 16 : 0u) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
-}
 // Instruction descriptor: fp32 accumulator, bf16 A and B, both K-major, M x N.
 __host__ __device__ constexpr uint32_t instr_desc(int M, int N) {
     return (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);

@@ -109,12 +109,6 @@ __device__ __forceinline__ void load_bulk_hint(void* dst, const void* src, uint3
         "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes.L2::cache_hint [%0], [%1], %2, [%3], %4;\n"
         ::"r"(smem_u32(dst)), "l"(src), "r"(bytes), "r"(smem_u32(bar)), "l"(policy) : "memory");
 }
-__device__ __forceinline__ void load_4d_hint(void* dst, const CUtensorMap* map, int x, int y, int z, int u, uint64_t* bar, uint64_t policy) {
-    asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.L2::cache_hint"
-        " [%0], [%1, {%3, %4, %5, %6}], [%2], %7;\n"
-        ::"r"(smem_u32(dst)), "l"(map), "r"(smem_u32(bar)), "r"(x), "r"(y), "r"(z), "r"(u), "l"(policy) : "memory");
-}
 __device__ __forceinline__ void load_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar) {
     asm volatile(
         "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];\n"
@@ -182,19 +176,6 @@ inline bool encode_bf16_3d(CUtensorMap* out, const void* base, uint64_t inner, u
     cuuint32_t estr[3] = {1, 1, 1};
     return fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, estr,
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-// Bytes [dim3][dim2][dim1][64], boxes of whole slabs of dim3 under the 64-byte swizzle.
-inline bool encode_u8_4d(CUtensorMap* out, const void* base, uint64_t d1, uint64_t d2, uint64_t d3, uint64_t stride1, uint64_t stride2, uint64_t stride3) {
-    EncodeFn fn = encoder();
-    if (!fn) return false;
-    cuuint64_t dims[4] = {64, d1, d2, d3};
-    cuuint64_t strides[3] = {stride1, stride2, stride3};
-    cuuint32_t box[4] = {64, (cuuint32_t)d1, (cuuint32_t)d2, 1};
-    cuuint32_t estr[4] = {1, 1, 1, 1};
-    return fn(out, CU_TENSOR_MAP_DATA_TYPE_UINT8, 4, const_cast<void*>(base), dims, strides, box, estr,
-              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
