@@ -739,6 +739,17 @@ def vector_decode_attn_q4(shape: Shape, q, cache: Q4Cache, W, out, ws=None, stre
 
 
 # ---- the mixed cache in 8 bits and pages
+def _on_current_device(*tensors):
+    """The calls run on the current device: a tensor of another one is refused."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def _of_cache(cache: Q8Cache):
+    return cache.ret_pages, cache.apx_pages, cache.ret_table, cache.apx_table, cache.ret_len, cache.apx_len, cache.ret_pos, cache.apx_pos
+
+
 def _q8(shape: Shape, cache: Q8Cache) -> bytes:
     """The cache's struct, its tensors checked: all calls but attention of one tier read its table and lengths, so both are."""
     return _q4(shape, cache, True, vector_q8_tile_bytes(shape), VECTOR_Q8_PAGE_ROWS)
@@ -791,6 +802,7 @@ def vector_compact_q8(shape: Shape, budget: Budget, K, V, ret_idx, apx_idx, cach
         if rc:
             _check(rc, "vector_compact_q8")
         return
+    _on_current_device(K, V, ret_idx, apx_idx, *_of_cache(cache))
     U, d = shape.units, shape.head_dim
     rc = load_library().vector_compact_q8(shape._p(), budget._p(), _sized(K, shape.torch_dtype, U * budget.n_tokens * d, "K"),
                                           _sized(V, shape.torch_dtype, U * budget.n_tokens * d, "V"),
@@ -806,6 +818,7 @@ def vector_append_q8(shape: Shape, cache: Q8Cache, k_new, v_new, first_row, pos=
         if rc:
             _check(rc, "vector_append_q8")
         return
+    _on_current_device(k_new, v_new, first_row, pos, *_of_cache(cache))
     B, width = shape.batch, shape.n_layers * shape.n_kv_heads * shape.head_dim
     n = k_new.numel() // (B * width)
     (kp, ks), (vp, vs) = _rows(k_new, shape.torch_dtype, B * n, width, "k_new"), _rows(v_new, shape.torch_dtype, B * n, width, "v_new")
@@ -821,7 +834,13 @@ def vector_read_q8(shape: Shape, cache: Q8Cache, ret_k=None, ret_v=None, apx_k=N
         if rc:
             _check(rc, "vector_read_q8")
         return
+    _on_current_device(ret_k, ret_v, apx_k, *_of_cache(cache))
     each, dt = shape.units * shape.head_dim, shape.torch_dtype
+    for t, name in ((ret_k, "ret_k"), (ret_v, "ret_v"), (apx_k, "apx_k")):
+        if t is not None and t.numel() % each:
+            raise ValueError(f"{name} must be [{shape.units}][n][{shape.head_dim}], got {tuple(t.shape)}")
+    if (ret_k is None) != (ret_v is None) or (ret_k is not None and ret_k.numel() != ret_v.numel()):
+        raise ValueError("ret_k and ret_v must have the same rows")
     n_ret, n_apx = (0 if t is None else t.numel() // each for t in (ret_k, apx_k))
     rc = load_library().vector_read_q8(shape._p(), _q8(shape, cache), n_ret, _sized(ret_k, dt, each * n_ret, "ret_k"), _sized(ret_v, dt, each * n_ret, "ret_v"),
                                        n_apx, _sized(apx_k, dt, each * n_apx, "apx_k"), _stream(stream))
@@ -838,6 +857,7 @@ def vector_decode_attn_q8(shape: Shape, q, cache: Q8Cache, W, out, ws=None, stre
         if rc:
             _check(rc, "vector_decode_attn_q8")
         return
+    _on_current_device(q, W, out, ws, *_of_cache(cache))
     wp, wn = _ws(ws)
     if out.dtype not in (torch.float32, torch.bfloat16):
         raise ValueError("out must be fp32 or bf16")
@@ -858,6 +878,7 @@ def vector_norm_rope(shape: Shape, n_tokens: int, q=None, k=None, v=None, q_out=
         if rc:
             _check(rc, "vector_norm_rope")
         return
+    _on_current_device(q, k, v, q_out, k_out, v_out, q_weight, k_weight, pos)
     d, dt, L, BL = shape.head_dim, shape.torch_dtype, shape.n_layers, shape.batch * shape.n_layers
     if not 0 <= q_first <= n_tokens:
         raise ValueError(f"q_first must lie in [0, {n_tokens}], got {q_first}")

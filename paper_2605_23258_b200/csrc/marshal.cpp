@@ -76,6 +76,8 @@ at::ScalarType type_of(const vector_shape& s) { return s.dtype == VECTOR_BF16 ? 
 // Reads a call's arguments.  `plain` turns false at the first one that is not: what is read from then on is nothing and means nothing.
 struct Reader {
     bool plain = true;
+    int here = -1;                                      // the device that tensors have to lie on, where the call asks for it
+    void on_current_device() { here = c10::cuda::current_device(); }
     bool need(bool holds) { return plain = plain && holds; }
     PyObject* attr(PyObject* o, Name n) {               // new, or null
         PyObject* v = plain ? PyObject_GetAttr(o, name[n]) : nullptr;
@@ -116,7 +118,7 @@ struct Reader {
     const at::Tensor* tensor(PyObject* o) { return need(o && THPVariable_CheckExact(o)) ? &THPVariable_Unpack(o) : nullptr; }
     void* device(PyObject* o, at::ScalarType type) {
         const at::Tensor* t = tensor(o);
-        return t && need(t->is_cuda() && t->is_contiguous() && t->scalar_type() == type) ? t->data_ptr() : nullptr;
+        return t && need(t->is_cuda() && t->is_contiguous() && t->scalar_type() == type && (here < 0 || t->get_device() == here)) ? t->data_ptr() : nullptr;
     }
     void* optional(PyObject* o, at::ScalarType type) { return o == Py_None ? nullptr : device(o, type); }
     // A tensor of n elements at least; null where there are none to have.
@@ -203,7 +205,7 @@ struct Reader {
     Rows rows(PyObject* o, at::ScalarType type, int64_t count, int64_t width) {
         Rows r;
         const at::Tensor* t = tensor(o);
-        if (!t || !need(t->is_cuda() && t->scalar_type() == type && width > 0 && t->numel() == count * width)) return r;
+        if (!t || !need(t->is_cuda() && t->scalar_type() == type && (here < 0 || t->get_device() == here) && width > 0 && t->numel() == count * width)) return r;
         r.p = t->data_ptr();
         r.stride = width;
         if (t->is_contiguous()) return r;
@@ -476,6 +478,7 @@ METHOD(decode_attn_q4) {                                // shape, q, cache, W, o
 }
 METHOD(compact_q8) {                                    // shape, budget, K, V, ret_idx, apx_idx, cache, stream
     return plain(n, 8, [&](Reader& r) {
+        r.on_current_device();
         const vector_shape s = r.shape(a[0]);
         const vector_budget b = r.budget(a[1]);
         const int64_t U = units_of(s), rows = U * b.n_tokens * s.head_dim;
@@ -488,6 +491,7 @@ METHOD(compact_q8) {                                    // shape, budget, K, V, 
 }
 METHOD(append_q8) {                                     // shape, cache, k_new, v_new, first_row, pos, rotate, stream
     return plain(n, 8, [&](Reader& r) {
+        r.on_current_device();
         const vector_shape s = r.shape(a[0]);
         const vector_q8_cache c = r.q8_cache(a[1], s);
         const int64_t width = (int64_t)s.n_layers * s.n_kv_heads * s.head_dim, each = width * s.batch;
@@ -502,11 +506,13 @@ METHOD(append_q8) {                                     // shape, cache, k_new, 
 }
 METHOD(read_q8) {                                       // shape, cache, ret_k, ret_v, apx_k, stream
     return plain(n, 6, [&](Reader& r) {
+        r.on_current_device();
         const vector_shape s = r.shape(a[0]);
         const vector_q8_cache c = r.q8_cache(a[1], s);
         const int64_t each = units_of(s) * s.head_dim;
         if (!r.need(each > 0)) return 0L;
         const int64_t n_ret = r.numel(a[2]) / each, n_apx = r.numel(a[4]) / each;
+        r.need(r.numel(a[2]) % each == 0 && r.numel(a[3]) == r.numel(a[2]) && (a[3] == Py_None) == (a[2] == Py_None) && r.numel(a[4]) % each == 0);
         void *rk = r.sized(a[2], type_of(s), n_ret * each), *rv = r.sized(a[3], type_of(s), n_ret * each), *ak = r.sized(a[4], type_of(s), n_apx * each);
         void* st = r.stream(a[5]);
         return run(r, [&] { return p_vector_read_q8(&s, &c, n_ret, rk, rv, n_apx, ak, st); });
@@ -514,6 +520,7 @@ METHOD(read_q8) {                                       // shape, cache, ret_k, 
 }
 METHOD(decode_attn_q8) {                                // shape, q, cache, W, out, ws, stream
     return plain(n, 7, [&](Reader& r) {
+        r.on_current_device();
         const vector_shape s = r.shape(a[0]);
         if (!r.need(s.n_kv_heads > 0)) return 0L;
         const int64_t rows = units_of(s) * (s.n_q_heads / s.n_kv_heads) * s.head_dim;
@@ -529,6 +536,7 @@ METHOD(decode_attn_q8) {                                // shape, q, cache, W, o
 }
 METHOD(norm_rope) {                                     // shape, n_tokens, q, k, v, q_out, k_out, v_out, q_weight, k_weight, pos, q_first, eps, stream
     return plain(n, 14, [&](Reader& r) {
+        r.on_current_device();
         const vector_shape s = r.shape(a[0]);
         const int64_t N = r.integer(a[1]), first = r.integer(a[11]), BL = (int64_t)s.batch * s.n_layers, d = s.head_dim;
         if (!r.need(s.batch > 0 && s.n_layers > 0 && s.n_q_heads > 0 && s.n_kv_heads > 0 && d > 0 && N > 0 && N <= (1 << 30) && first >= 0 && first <= N && PyFloat_Check(a[12]))) return 0L;

@@ -172,11 +172,12 @@ def test_rows_that_are_not_given_or_have_no_place():
     assert np.array_equal(k[4, :4], plain.rounded(x[4, :4, 0].double().numpy()))     # counted from row 0
 
 
+@pytest.mark.parametrize("LH", [2, 3])                       # heads that share a thread block by two, and alone
 @pytest.mark.parametrize("dtype,d", [(BF, 128), (BF, 64), (F32, 128), (F32, 64)])
-def test_keys_are_turned_on_the_way(dtype, d):
+def test_keys_are_turned_on_the_way(dtype, d, LH):
     """Within half a step of the turned key in 64 bits, and what fp32 makes of it: sine and cosine (2^-24 and 2e-9 of angle and series), two products and a sum."""
     rng = np.random.default_rng(d)
-    B, LH, n = 3, 2, 45
+    B, n = 3, 45
     sh = _shape(B, 1, LH, d, dtype, 1)
     c = _cache(sh, 70, 0, 3)
     c.ret_len[:], first = _ints([45, 60, 64]), np.array([0, 20, 31])
@@ -262,6 +263,10 @@ def test_refusals_of_the_binding():
         vec.vector_append_q8(sh, c, x, x, _ints([0, 0]))
     with pytest.raises(vec.VectorError, match="shape"):
         vec.vector_append_q8(sh, c, x, x, _ints([0, 0]), _ints([[0] * 3] * 2), rotate=True)
+    out = torch.zeros(4, 3, 128, dtype=BF, device=DEV)
+    for k, v in ((out, None), (None, out), (out, out[:, :2].contiguous()), (out.flatten()[:-1], out.flatten()[:-1]), (out.float(), out.float()), (out.cpu(), out.cpu())):
+        with pytest.raises(ValueError):
+            vec.vector_read_q8(sh, c, k, v)
     four = vec.alloc_q4_cache(sh, 4, 4, 2, 2)
     with pytest.raises(ValueError, match="pages"):
         vec.vector_read_q8(sh, four, torch.zeros(4, 3, 128, dtype=BF, device=DEV), torch.zeros(4, 3, 128, dtype=BF, device=DEV))
