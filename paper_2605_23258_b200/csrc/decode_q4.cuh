@@ -106,11 +106,13 @@ template <typename Cost> __device__ __forceinline__ int tile_from(int64_t r, int
 // FOLD: EXACT with at most four heads, whose first and second parts of weights are eight columns of one product.
 template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> struct Cfg {
     static_assert(EXACT || !FOLD, "one part needs no folding");
-    static constexpr int WARPS = EXACT && D == 128 && (!FOLD || ROPE || sizeof(T) == 4) ? 8 : 12;
+    // 8 bits, us by 12 warps and by 16, which have 128 registers a thread: 64 channels, 512 units of up to 1700 and 3300 rows, fp32 results 51.2 and 46.5, bf16 48.4 and 45.0, rotary keys (472
+    // units) 40.1 and 36.6; 128 channels 227 and 302.
+    static constexpr int WARPS = EXACT && D == 128 && (!FOLD || ROPE || sizeof(T) == 4) ? 8 : F::SCALED && D == 64 ? 16 : 12;
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int POS_AT = F::template TILE<D>;                 // of a key-only tile's positions, within an entry
     static constexpr int ENTRY_BYTES = F::template TILE<D> + (ROPE ? 4 * F::ROWS : 0);
-    static constexpr int ENTRIES = WARPS == 12 ? 3 : 4;                // of a warp's ring, a tile each
+    static constexpr int ENTRIES = WARPS == 8 ? 4 : 3;                // of a warp's ring, a tile each
     static constexpr int SMEM_BYTES = WARPS * ENTRIES * ENTRY_BYTES;   // and behind them the prefix sums
     static constexpr int Q_PARTS = sizeof(T) == 4 ? 2 : 1;
     // Rows that may be turned are taken halved: a pair of stored channels, 61440 each, turns to 86889 at the most, and half of that is within fp16's 65504.
