@@ -502,7 +502,7 @@ VECTOR_API size_t vector_decode_q8_workspace_bytes(const vector_shape* shape);
  * vector_decode_attn_q4 over the 8-bit pages: the same arguments, lengths read on the device, the same answers where rows are missing, and the same arithmetic: products of
  * stored rows are exact, sums fp32, weights and turned keys in fp16 (in two parts with fp32 queries or output).  The scale of a block's keys is a factor of its logits, that of its
  * values (and of key-only keys) one of the sums, which hold for the scale of the block before and change to the next one's.  A NaN in a key makes its unit's outputs NaN, one in a
- * value that channel's.
+ * value that channel's.  ws: at least vector_decode_q8_workspace_bytes() at a multiple of 256 bytes; calls that overlap on the GPU, two captured graphs' too, need workspaces of their own.
  */
 VECTOR_API vector_status vector_decode_attn_q8(const vector_shape* shape, const void* q, const vector_q8_cache* cache, const void* W,
                                                void* out, int32_t out_dtype, void* ws, size_t ws_bytes, void* stream);

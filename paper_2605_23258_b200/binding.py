@@ -781,6 +781,13 @@ def _rows(t, dtype, rows: int, width: int, name: str):
     return t.data_ptr(), step
 
 
+def _positions(pos, n: int):
+    """Positions of n tokens, no more: those of wider rows would be other tokens'."""
+    if pos is not None and pos.numel() != n:
+        raise ValueError(f"pos must have {n} elements, got {tuple(pos.shape)}")
+    return None if pos is None else _sized(pos, torch.int32, n, "pos")
+
+
 def vector_q8_tile_bytes(shape: Shape) -> int:
     """Bytes of a page's 32 rows of one (layer, KV head)."""
     return int(load_library().vector_q8_tile_bytes(shape._p()))
@@ -823,7 +830,7 @@ def vector_append_q8(shape: Shape, cache: Q8Cache, k_new, v_new, first_row, pos=
     n = k_new.numel() // (B * width)
     (kp, ks), (vp, vs) = _rows(k_new, shape.torch_dtype, B * n, width, "k_new"), _rows(v_new, shape.torch_dtype, B * n, width, "v_new")
     rc = load_library().vector_append_q8(shape._p(), _q8(shape, cache), kp, ks, vp, vs, n, _sized(first_row, torch.int32, B, "first_row"),
-                                         None if pos is None else _sized(pos, torch.int32, B * n, "pos"), int(rotate), _stream(stream))
+                                         _positions(pos, B * n), int(rotate), _stream(stream))
     _check(rc, "vector_append_q8")
 
 
@@ -887,7 +894,7 @@ def vector_norm_rope(shape: Shape, n_tokens: int, q=None, k=None, v=None, q_out=
         part[name] = (None, 0, None) if t is None else (*_rows(t, dt, BL * n_tokens, heads * d, name), _sized(out, dt, BL * heads * (n_tokens - first) * d, name + "_out"))
     wq, wk = (None if w is None else _sized(w, dt, L * d, name) for w, name in ((q_weight, "q_weight"), (k_weight, "k_weight")))
     rc = load_library().vector_norm_rope(shape._p(), n_tokens, part["q"][0], part["q"][1], wq, q_first, part["q"][2], part["k"][0], part["k"][1], wk, part["k"][2],
-                                         *part["v"], None if pos is None else _sized(pos, torch.int32, shape.batch * n_tokens, "pos"), eps, _stream(stream))
+                                         *part["v"], _positions(pos, shape.batch * n_tokens), eps, _stream(stream))
     _check(rc, "vector_norm_rope")
 
 

@@ -499,6 +499,7 @@ METHOD(append_q8) {                                     // shape, cache, k_new, 
         const int64_t rows = r.numel(a[2]) / each;
         const Reader::Rows k = r.rows(a[2], type_of(s), s.batch * rows, width), v = r.rows(a[3], type_of(s), s.batch * rows, width);
         const int32_t *first = r.ints(a[4], s.batch), *pos = r.optional_ints(a[5], s.batch * rows);
+        r.need(a[5] == Py_None || r.numel(a[5]) == s.batch * rows);
         const int32_t rotate = a[6] == Py_True;
         void* st = r.stream(a[7]);
         return run(r, [&] { return p_vector_append_q8(&s, &c, k.p, k.stride, v.p, v.stride, rows, first, pos, rotate, st); });
@@ -552,6 +553,7 @@ METHOD(norm_rope) {                                     // shape, n_tokens, q, k
         void* weight[2];
         for (int i = 0; i < 2; ++i) weight[i] = a[8 + i] == Py_None ? nullptr : r.sized(a[8 + i], type, s.n_layers * d);
         const int32_t* pos = r.optional_ints(a[10], s.batch * N);
+        r.need(a[10] == Py_None || r.numel(a[10]) == s.batch * N);
         const float eps = (float)PyFloat_AsDouble(a[12]);
         void* st = r.stream(a[13]);
         return run(r, [&] {

@@ -5,7 +5,7 @@
 //
 // A group of D / E lanes has a token and a run of heads of one projection, 16 bytes of a row a lane, several rows on their way at once: the factors of a channel, w cos t and (of the
 // pair's other channel, with its sign) w sin t, are computed once for the run, and a row then takes a sum of squares over its lanes, one exchange of its raw bytes with the lane half a
-// head away, two products and a factor a channel, two channels an instruction.  All in fp32, rounded once.  Bound by memory where there are many tokens (0.89 to 0.95 of the copy rate), by one
+// head away, two products and a factor a channel, two channels an instruction.  All in fp32, rounded once.  Bound by memory where there are many tokens (0.87 to 0.95 of the copy rate), by one
 // launch and the chain load, sum, store where there are few (64 tokens 3.4 us).
 #include "common.cuh"
 #include "internal.h"

@@ -226,8 +226,7 @@ class PagedCache:
                     raise ValueError(f"{name}: rows must lie at multiples of 16 bytes")
             if pos is None and (rotate or self.cache.ret_pos is not None):
                 raise ValueError("pos is missing")
-            if pos is not None:
-                B._sized(pos, torch.int32, sh.batch * n, "pos")
+            B._positions(pos, sh.batch * n)
             self._change("ret", self.active if n == 1 else self.active * n)
             B.vector_append_q8(self.shape, self.cache, k_new, v_new, self.first_row, pos, rotate)
             return

@@ -136,7 +136,7 @@ def test_both_ways_of_marshalling_and_streams(monkeypatch):
     plain = _run(sh, 21, qkv, 4, w, pos)
     for x in (dense, heads, other, plain):
         assert all(torch.equal(first[n], x[n]) for n in first)
-    for bad in (dict(q=qkv[0][..., :-128]), dict(k_weight=w[1].float()), dict(pos=pos[:2]), dict(q_out=first["q"][:2]), dict(v=qkv[2].transpose(0, 2)), dict(q_first=22)):
+    for bad in (dict(q=qkv[0][..., :-128]), dict(k_weight=w[1].float()), dict(pos=pos[:2]), dict(pos=torch.cat([pos, pos], 1)), dict(q_out=first["q"][:2]), dict(v=qkv[2].transpose(0, 2)), dict(q_first=22)):
         kw = dict(q=qkv[0], k=qkv[1], v=qkv[2], q_out=first["q"], k_out=first["k"], v_out=first["v"], q_weight=w[0], k_weight=w[1], pos=pos, q_first=4)
         kw.update(bad)
         with pytest.raises(ValueError):

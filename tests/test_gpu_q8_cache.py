@@ -256,7 +256,7 @@ def test_refusals_of_the_binding():
     sh = _shape(2, 1, 2, 128, BF)
     c = _cache(sh, 64, 32, 1)
     x = torch.zeros(2, 3, 2, 128, dtype=BF, device=DEV)
-    for bad in (dict(k=x.float()), dict(v=x[:, :2]), dict(first=_ints([0])), dict(pos=_ints([0, 1])), dict(k=x.transpose(1, 2))):
+    for bad in (dict(k=x.float()), dict(v=x[:, :2]), dict(first=_ints([0])), dict(pos=_ints([0, 1])), dict(pos=_ints([[0] * 4] * 2)), dict(k=x.transpose(1, 2))):
         with pytest.raises(ValueError):
             vec.vector_append_q8(sh, c, bad.get("k", x), bad.get("v", x), bad.get("first", _ints([0, 0])), bad.get("pos", _ints([[0] * 3] * 2)))
     with pytest.raises(vec.VectorError, match="null"):
