@@ -205,3 +205,81 @@ def test_offsets_beyond_32_bits():
     out = plain.decode(sh, q, c, W, F32)
     o, *sizes = q4_plain.attend(q[0].double().cpu().numpy(), *want, W[0].double().cpu().numpy(), 128 ** -0.5)
     assert np.all(np.abs(out[0].double().cpu().numpy() - o) <= q4_plain.tolerance(o, *sizes, BF, F32, False))
+
+
+def _shared(batch, g, d, dtype, rk, rv, q, sm_scale):
+    """`batch` sequences that share the pages of rows rk, rv, which are held exactly."""
+    n = len(rk)
+    shape = vec.Shape(batch, 1, g, 1, d, vec.VECTOR_BF16 if dtype == BF else vec.VECTOR_F32, 16, 7, sm_scale, 0, 10000.0)
+    pages = -(-n // 32)
+    pool = np.zeros((pages, 1, 2 * plain.tile_bytes(d)), np.uint8)
+    for which, x in ((0, rk), (1, rv)):
+        plain.put_rows(pool, np.arange(pages), 0, which, x)
+        assert np.array_equal(plain.row_values(pool, np.arange(pages), range(n), 0, which, d), x)
+    ints = lambda x: torch.as_tensor(x, dtype=torch.int32, device="cuda")  # noqa: E731
+    c = vec.Q8Cache(torch.from_numpy(pool).cuda(), torch.empty(0, 1, plain.tile_bytes(d), dtype=torch.uint8, device="cuda"), ints(np.tile(np.arange(pages), (batch, 1))),
+                    torch.empty(batch, 0, dtype=torch.int32, device="cuda"), ints(np.full(batch, n)), ints(np.zeros(batch)))
+    return shape, torch.from_numpy(q).to(dtype).cuda().expand(batch, g, d).contiguous(), c, torch.zeros(1, d, d, dtype=dtype, device="cuda")
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("d,g", [(128, 4), (64, 4), (128, 8), (64, 1)])
+@pytest.mark.parametrize("gap", [8, 14, 18])
+def test_a_sink_without_a_value(dtype, out_dtype, d, g, gap):
+    """A key that takes all the weight and has a value of zero, before thousands whose weights are e^-gap of it and make the output, with values whose blocks' scales go up and down.  Tolerance as over
+    the 4-bit pages: logits are exact but for the factor (2^-23 twice of gap, twice), exponentials 2^-21 twice, weights 2^-11 twice in one fp16 part and 2^-21 twice in two, sums of 16 rows 2^-20 and
+    n / 16 of these 2^-24 each, twice (2^-23 where they are cut off), and the result's own rounding."""
+    n = 3500
+    rng = np.random.default_rng(gap)
+    rk, rv = np.zeros((n, d)), rng.choice([0.5, 1.0, 1.5, 2.0, 3.0], (n, d)) * np.repeat(2.0 ** rng.integers(-6, 7, -(-n // 32)), 32)[:n, None]
+    rk[1:, 5], rk[:, 4] = -2.0, 3.0
+    rv[0] = 0
+    q = np.zeros((g, d))
+    q[:, 5] = 1.0
+    sh, qt, c, W = _shared(1000, g, d, dtype, rk, rv, q, gap / 2.0)
+    out = plain.decode(sh, qt, c, W, out_dtype).double().cpu().numpy()
+    p = np.exp(-float(gap))
+    o = (p * rv[1:].sum(0) / (1 + (n - 1) * p))[None, None]
+    exact = F32 in (dtype, out_dtype)
+    steps = -(-n // 16) * (2.0 ** -24 if exact else 2.0 ** -23)
+    tol = (gap * 2.0 ** -23 * 2 + 2.0 ** -20 + (2.0 ** -20 if exact else 2.0 ** -10) + 2.0 ** -20 + 2 * steps + (2.0 ** -24 if out_dtype == F32 else 2.0 ** -8)) * o
+    err = np.abs(out - o)
+    assert np.all(err <= tol), float((err / tol).max())
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("d,g,top", [(128, 4, 1 << 20), (64, 3, 1 << 30), (128, 2, 1 << 30), (64, 8, 1 << 30)])
+def test_far_positions(dtype, out_dtype, d, g, top):
+    """Positions up to 2^30: the tolerance is that of near ones."""
+    sh, q, c, W = plain.problem(2, 1, 1, g, d, dtype, [(0, 200), (90, 65)], 32, rope=True)
+    c.apx_pos.copy_(torch.randint(top // 2, top, c.apx_pos.shape, generator=torch.Generator().manual_seed(1), dtype=torch.int32))
+    plain.check_decode(sh, q, c, W, plain.decode(sh, q, c, W, out_dtype), True)
+
+
+@pytest.mark.parametrize("dtype,out_dtype", [(BF, BF), (BF, F32), (F32, F32)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_largest_stored_keys_turned(dtype, out_dtype, d):
+    """Keys of 448 2^31 in every channel, whose pairs turn to 634 2^31: the even heads attend to one alone, for the odd ones its weight is zero.  No logit term in the tolerance of the even
+    heads, as the weights are one and zero."""
+    at, g = 37, 4
+    sh, q, c, W = plain.problem(1, 1, 1, g, d, dtype, [(70, 130)], 31, rope=True)
+    t, page = c.apx_table.cpu().numpy()[0], int(c.apx_table[0, at // 32])
+    pool = c.apx_pages.cpu().numpy()
+    x = np.zeros((32, d))
+    x[at % 32] = 448 * 2.0 ** 31
+    plain.put_rows(pool, [page], 0, 0, x)
+    c.apx_pages.copy_(torch.from_numpy(pool))
+    c.apx_pos[page, 0, at % 32] = 7854
+    q[0] = q[0].abs()
+    q[0, 1::2] *= -1
+    out = plain.decode(sh, q, c, W, out_dtype)
+    rows = np.arange(130)
+    ak, pos = plain.row_values(pool, t, rows, 0, 0, d), c.apx_pos.cpu().numpy()[t[rows // 32], 0, rows % 32]
+    rk, rv = (plain.row_values(c.ret_pages.cpu().numpy(), c.ret_table[0].cpu().numpy(), range(70), 0, w, d) for w in (0, 1))
+    none = np.zeros((0, d))
+    for heads, pick in ((slice(0, None, 2), rows == at), (slice(1, None, 2), rows != at)):
+        even = heads.start == 0
+        o, spread, logit, turned = q4_plain.attend(q[0, heads].double().cpu().numpy(), none if even else rk, none if even else rv, ak[pick], W[0].double().cpu().numpy(), d ** -0.5, pos[pick])
+        tol = q4_plain.tolerance(o, spread, logit * heads.start, turned, dtype, out_dtype, True)
+        err = np.abs(out[0, heads].double().cpu().numpy() - o)
+        assert np.all(np.isfinite(err)) and np.all(err <= tol), (heads.start, float((err / tol).max()))
