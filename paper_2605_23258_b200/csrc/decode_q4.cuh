@@ -129,7 +129,9 @@ template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> 
     // What tiles of the tiers cost, (retained, key-only).  us for 128 units of 3000 and 6000 rows, four heads, 128 channels and 64: (4, 3) 44 and 33, (1, 1) 47 and 35, (2, 1) 48 and
     // 34, (2, 3) 52 and 40; fp32 results 47 and 35, 50 and 37, 51 and 37, 55 and 42.  Rotary keys: (2, 3) 70.8 and 47.0, (1, 2) 70.3 and 52.6, (1, 1) 78 and 48, (4, 3) 81 and 49; fp32 results,
     // turned in two parts: (1, 2) 140 and 76, (2, 3) 150 and 80, (1, 1) 171 and 88, (4, 3) 189 and 91.  fp32 queries and eight heads order them alike.
-    using Cost = std::conditional_t<!ROPE, Costs<4, 3>, std::conditional_t<EXACT, Costs<1, 2>, Costs<2, 3>>>;
+    // 8 bits, rotary keys and 64 channels, 472 units of one ragged batch, 256 units of another and 128 of 3277 and 6552 rows: (4, 5) 34.8, 61.6 and 53.3, (2, 3) 36.6, 65.5 and 57.5, (1, 1) 35.6, 62.7 and 54.6,
+    // (5, 6) 34.9, 60.9 and 54.1; 128 channels, the first: (2, 3) 53.4, (4, 5) 55.0, (1, 1) 56.5, (1, 2) 58.4.  fp32 results, 64 channels, the first two: (1, 2) 51 and 97, (2, 3) 54 and 102, (1, 3) 57 and 112.
+    using Cost = std::conditional_t<!ROPE, Costs<4, 3>, std::conditional_t<EXACT, Costs<1, 2>, std::conditional_t<F::SCALED && D == 64, Costs<4, 5>, Costs<2, 3>>>>;
 };
 
 // Not volatile, like the transposes: the compiler may move them past one another, so that one's operands are on their way during the next.
