@@ -107,7 +107,7 @@ template <typename Cost> __device__ __forceinline__ int tile_from(int64_t r, int
 template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> struct Cfg {
     static_assert(EXACT || !FOLD, "one part needs no folding");
     // 8 bits, us by 12 warps and by 16, which have 128 registers a thread: 64 channels, 512 units of up to 1700 and 3300 rows, fp32 results 51.2 and 46.5, bf16 48.4 and 45.0, rotary keys (472
-    // units) 40.1 and 36.6; 128 channels 227 and 302.
+    // units, by the costs (2, 3)) 40.1 and 36.6; 128 channels 227 and 302.
     static constexpr int WARPS = EXACT && D == 128 && (!FOLD || ROPE || sizeof(T) == 4) ? 8 : F::SCALED && D == 64 ? 16 : 12;
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int POS_AT = F::template TILE<D>;                 // of a key-only tile's positions, within an entry
