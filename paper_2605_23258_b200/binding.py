@@ -756,7 +756,7 @@ def _q8(shape: Shape, cache: Q8Cache) -> bytes:
 
 
 def _rows(t, dtype, rows: int, width: int, name: str):
-    """Pointer and distance, in elements, of rows of `width` neighbouring elements each: the last dimensions of a tensor make up a row, the others count rows that lie evenly."""
+    """Pointer and distance, in elements, of rows of `width` neighbouring elements each: the last dimensions of a tensor make up a row, the others count rows that lie evenly and apart."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA tensor")
     if t.dtype != dtype:
@@ -778,6 +778,8 @@ def _rows(t, dtype, rows: int, width: int, name: str):
     for (_, outer), (n, inner) in zip(sizes[:at], sizes[1:at]):
         if outer != n * inner:
             raise ValueError(f"{name}: rows must lie evenly, got strides {t.stride()}")
+    if step < width:
+        raise ValueError(f"{name}: rows must lie apart, got strides {t.stride()}")
     return t.data_ptr(), step
 
 

@@ -38,7 +38,7 @@ def _stale() -> bool:
 def build_marshal(force: bool = False) -> str:
     """The extension module behind the binding (csrc/marshal.cpp): plain C++ against the headers of Python and torch."""
     src, target = os.path.join(CSRC, "marshal.cpp"), marshal_path()
-    if not force and not _older(target, [src]):
+    if not force and not _older(target, [src, os.path.join(CSRC, "rows.h")]):
         return target
     import shutil
     import sysconfig

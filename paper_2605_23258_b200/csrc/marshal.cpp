@@ -14,6 +14,7 @@
 
 #include <cmath>
 
+#include "rows.h"
 #include "vector.h"
 
 namespace {
@@ -200,7 +201,7 @@ struct Reader {
         c.n_apx = field(o, N_APX);
         return c;
     }
-    // Rows of `width` neighbouring elements: contiguous ones, or those of a tensor whose last dimension, or last two, make up a row of evenly lying ones.
+    // Rows of `width` neighbouring elements: contiguous ones, or those that rows.h finds.
     struct Rows { void* p = nullptr; int64_t stride = 0; };
     Rows rows(PyObject* o, at::ScalarType type, int64_t count, int64_t width) {
         Rows r;
@@ -208,22 +209,7 @@ struct Reader {
         if (!t || !need(t->is_cuda() && t->scalar_type() == type && (here < 0 || t->get_device() == here) && width > 0 && t->numel() == count * width)) return r;
         r.p = t->data_ptr();
         r.stride = width;
-        if (t->is_contiguous()) return r;
-        int64_t run = 1;
-        int at = (int)t->dim();
-        while (run < width) {
-            --at;
-            if (t->size(at) == 1) continue;
-            if (!need(t->stride(at) == run && width % (run * t->size(at)) == 0)) return r;
-            run *= t->size(at);
-        }
-        int64_t next = 0;                               // the distance of the next dimension's steps, 0: not known yet
-        while (--at >= 0) {
-            if (t->size(at) == 1) continue;
-            if (next == 0) r.stride = t->stride(at);
-            else if (!need(t->stride(at) == next)) return r;
-            next = t->stride(at) * t->size(at);
-        }
+        if (!t->is_contiguous()) need(vec::row_distance(t->sizes().data(), t->strides().data(), (int)t->dim(), width, &r.stride));
         return r;
     }
     vector_q4_cache q8_cache(PyObject* o, const vector_shape& s) { return q4_cache(o, s, true, p_vector_q8_tile_bytes, VECTOR_Q8_PAGE_ROWS); }
