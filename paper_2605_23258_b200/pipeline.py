@@ -170,6 +170,8 @@ class PagedCache:
         for t, name in ((K, "K"), (V, "V")):
             if B._sized(t, sh.torch_dtype, sh.units * b.n_tokens * sh.head_dim, name) % 16:
                 raise ValueError(f"{name} must lie at a multiple of 16 bytes")
+        if self.bits == 8:
+            B._on_current_device(K, V, comp.ret_idx, comp.apx_idx, *B._of_cache(c))
 
     def admit(self, place: int, comp: Compressor, K, V) -> torch.Tensor:
         """Takes the routed context of a Compressor of one sequence (its score and route have been called) to a place that is not taken.  Returns whether
@@ -227,6 +229,7 @@ class PagedCache:
             if pos is None and (rotate or self.cache.ret_pos is not None):
                 raise ValueError("pos is missing")
             B._positions(pos, sh.batch * n)
+            B._on_current_device(k_new, v_new, pos, *B._of_cache(self.cache))
             self._change("ret", self.active if n == 1 else self.active * n)
             B.vector_append_q8(self.shape, self.cache, k_new, v_new, self.first_row, pos, rotate)
             return
