@@ -480,7 +480,8 @@ VECTOR_API vector_status vector_compact_q8(const vector_shape* shape, const vect
  * New rows of every sequence's retained tier, from one generated token to a piece of a prompt, keys turned by their positions on the way.  ret_len[b] counts the new
  * rows already: rows first_row[b] .. ret_len[b] - 1 (first_row and ret_len: as vector_block_tables wrote them), n_new at the most, are k_new[b][0], k_new[b][1], ...; a sequence
  * with fewer has none of the others read.  k_new, v_new: device [batch][n_new] rows of L * Hkv * d elements, k_stride and v_stride elements apart, so that
- * they may be part of a wider row.  pos: device [batch][n_new], the tokens' positions; they go to ret_pos where that is not NULL (pos may be NULL where neither needs it).
+ * they may be part of a wider row (vector_norm_rope writes rows of this order, a token's heads behind one another, where its shape has a sequence a token: batch * n_new sequences of
+ * one layer and one token).  pos: device [batch][n_new], the tokens' positions; they go to ret_pos where that is not NULL (pos may be NULL where neither needs it).
  * rotate != 0 (needs shape->rope_enabled, else VECTOR_ERR_SHAPE): the pair of channels (c, c + d/2) is turned by pos theta^(-2c/d), in fp32, before it is rounded.
  * A new row that the scale of its block does not hold makes the scale larger, and the rows that are there are rounded again; the first row of a block begins a new scale.
  */

@@ -783,6 +783,14 @@ def _rows(t, dtype, rows: int, width: int, name: str):
     return t.data_ptr(), step
 
 
+def _new_rows(shape: Shape, n: int, t, name: str):
+    """_rows of n new tokens of every sequence.  [units][n][d], as vector_norm_rope writes a context, holds as many numbers in another order: several tokens have to show theirs."""
+    width = shape.n_layers * shape.n_kv_heads * shape.head_dim
+    if n > 1 and tuple(t.shape[:2]) != (shape.batch, n) and tuple(t.shape) != (shape.batch * n, width):
+        raise ValueError(f"{name} must be [{shape.batch}][{n}] rows of all layers' and heads' channels, got {tuple(t.shape)}")
+    return _rows(t, shape.torch_dtype, shape.batch * n, width, name)
+
+
 def _positions(pos, n: int):
     """Positions of n tokens, no more: those of wider rows would be other tokens'."""
     if pos is not None and pos.numel() != n:
@@ -821,7 +829,9 @@ def vector_compact_q8(shape: Shape, budget: Budget, K, V, ret_idx, apx_idx, cach
 
 
 def vector_append_q8(shape: Shape, cache: Q8Cache, k_new, v_new, first_row, pos=None, rotate: bool = False, stream=None):
-    """k_new, v_new [batch][n] rows of L * Hkv * d elements: rows first_row[b] .. cache.ret_len[b] - 1 of every sequence, keys turned by pos [batch][n] where `rotate`."""
+    """k_new, v_new [batch][n] rows of L * Hkv * d elements: rows first_row[b] .. cache.ret_len[b] - 1 of every sequence, keys turned by pos [batch][n] where `rotate`.
+    Of several tokens the first two dimensions are [batch][n], or the only two [batch * n][L * Hkv * d].  vector_norm_rope leaves rows of this order where its shape has a sequence a token
+    (batch * n sequences of one layer and one token, pos [batch * n])."""
     rc = (_marshal_module or _marshal()).append_q8(shape, cache, k_new, v_new, first_row, pos, rotate, _handle(stream))
     if rc is not None:
         if rc:
@@ -830,7 +840,7 @@ def vector_append_q8(shape: Shape, cache: Q8Cache, k_new, v_new, first_row, pos=
     _on_current_device(k_new, v_new, first_row, pos, *_of_cache(cache))
     B, width = shape.batch, shape.n_layers * shape.n_kv_heads * shape.head_dim
     n = k_new.numel() // (B * width)
-    (kp, ks), (vp, vs) = _rows(k_new, shape.torch_dtype, B * n, width, "k_new"), _rows(v_new, shape.torch_dtype, B * n, width, "v_new")
+    (kp, ks), (vp, vs) = _new_rows(shape, n, k_new, "k_new"), _new_rows(shape, n, v_new, "v_new")
     rc = load_library().vector_append_q8(shape._p(), _q8(shape, cache), kp, ks, vp, vs, n, _sized(first_row, torch.int32, B, "first_row"),
                                          _positions(pos, B * n), int(rotate), _stream(stream))
     _check(rc, "vector_append_q8")

@@ -483,6 +483,10 @@ METHOD(append_q8) {                                     // shape, cache, k_new, 
         const int64_t width = (int64_t)s.n_layers * s.n_kv_heads * s.head_dim, each = width * s.batch;
         if (!r.need(each > 0 && width > 0 && PyBool_Check(a[6]))) return 0L;
         const int64_t rows = r.numel(a[2]) / each;
+        for (PyObject* o : {a[2], a[3]}) {               // several tokens have to show their order
+            const at::Tensor* t = r.tensor(o);
+            r.need(t && (rows <= 1 || (t->dim() >= 2 && ((t->size(0) == s.batch && t->size(1) == rows) || (t->dim() == 2 && t->size(0) == s.batch * rows && t->size(1) == width)))));
+        }
         const Reader::Rows k = r.rows(a[2], type_of(s), s.batch * rows, width), v = r.rows(a[3], type_of(s), s.batch * rows, width);
         const int32_t *first = r.ints(a[4], s.batch), *pos = r.optional_ints(a[5], s.batch * rows);
         r.need(a[5] == Py_None || r.numel(a[5]) == s.batch * rows);

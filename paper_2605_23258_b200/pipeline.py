@@ -215,15 +215,15 @@ class PagedCache:
 
     def append(self, k_new, v_new, pos, rotate: bool = False):
         """A generated token of every active place: k_new, v_new [U][d], pos [batch] int32.  A request that finds no page left keeps its length.
-        8 bits: or n tokens, [batch][n] rows of all layers' and heads' channels with pos [batch][n], of which a request that finds too few pages keeps the first ones; rotate: the keys are
-        still to be turned by their positions."""
+        8 bits: or n tokens, [batch][n] rows of all layers' and heads' channels with pos [batch][n] (vector_append_q8 says how they come from projections), of which a request that finds too few
+        pages keeps the first ones; rotate: the keys are still to be turned by their positions."""
         if self.bits == 8:
             sh = self.shape                                 # what is refused is refused before the tables change
-            width, n = sh.n_layers * sh.n_kv_heads * sh.head_dim, k_new.numel() // (sh.units * sh.head_dim)
+            n = k_new.numel() // (sh.units * sh.head_dim)
             if rotate and not sh.rope_enabled:
                 raise ValueError("keys are turned where the shape has rotary positions")
             for t, name in ((k_new, "k_new"), (v_new, "v_new")):
-                at, stride = B._rows(t, sh.torch_dtype, sh.batch * n, width, name)
+                at, stride = B._new_rows(sh, n, t, name)
                 if at % 16 or stride * t.element_size() % 16:
                     raise ValueError(f"{name}: rows must lie at multiples of 16 bytes")
             if pos is None and (rotate or self.cache.ret_pos is not None):
