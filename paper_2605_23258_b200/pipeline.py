@@ -209,7 +209,10 @@ class PagedCache:
         self._taken.difference_update(at)
 
     def project(self, q, k, v, q_weight=None, k_weight=None, pos=None, eps: float = 1e-6):
-        """The layers' projections of one token of every place, [B][L] rows, as the rows of append and decode: q [U][g][d], k and v [U][d]."""
+        """The layers' projections of one token of every place, [B][L] rows, as the rows of append and decode: q [U][g][d], k and v [U][d].  pos [batch], the tokens' positions, is needed where
+        the shape has rotary ones: queries and keys come turned by it, so that append takes them without rotate."""
+        if self.shape.rope_enabled and pos is None:
+            raise ValueError("pos is missing: queries and keys are turned by the tokens' positions")
         q, k, v = project(self.shape, 1, q, k, v, q_weight, k_weight, pos, eps)
         return q[:, :, 0], k[:, 0], v[:, 0]
 
