@@ -84,13 +84,16 @@ struct Deal {
     int64_t X;
     int workers;
     double step;                    // 0: few tiles
-    __device__ __forceinline__ Deal(int64_t x, int workers_at_most, int most_cost) : X(x), workers(workers_at_most), step(0.) {
+    __host__ __device__ __forceinline__ Deal(int64_t x, int workers_at_most, int most_cost) : X(x), workers(workers_at_most), step(0.) {
         if (x > (int64_t)workers_at_most * (most_cost + 1)) step = (double)x / workers_at_most;
         else workers = max(min((int)x / most_cost, workers_at_most), 1);
     }
-    __device__ __forceinline__ int64_t begin(int w) const {
+    __host__ __device__ __forceinline__ int64_t begin(int w) const {
         if (w == workers) return X;
-        return step > 0. ? (int64_t)(step * w) : (int64_t)((uint32_t)X * (uint32_t)w / (uint32_t)workers);      // under 2^32: X is at most some hundred times the workers there
+        if (step > 0.) return (int64_t)(step * w);
+        // X w / workers.  X is up to 750 times the workers there, and the product not always under 2^32: the quotient and what it leaves are.
+        const uint32_t n = (uint32_t)workers, whole = (uint32_t)X / n, rest = (uint32_t)X - whole * n;
+        return (int64_t)(whole * (uint32_t)w + rest * (uint32_t)w / n);
     }
 };
 // a / b, in 32 bits where they do.
