@@ -477,13 +477,17 @@ VECTOR_API vector_status vector_compact_q8(const vector_shape* shape, const vect
                                            const int32_t* ret_idx, const int32_t* apx_idx, const vector_q8_cache* cache, void* stream);
 
 /*
- * New rows of every sequence's retained tier, from one generated token to a piece of a prompt, keys turned by their positions on the way.  ret_len[b] counts the new
- * rows already: rows first_row[b] .. ret_len[b] - 1 (first_row and ret_len: as vector_block_tables wrote them), n_new at the most, are k_new[b][0], k_new[b][1], ...; a sequence
- * with fewer has none of the others read.  k_new, v_new: device [batch][n_new] rows of L * Hkv * d elements, k_stride and v_stride elements apart, so that
- * they may be part of a wider row (vector_norm_rope writes rows of this order, a token's heads behind one another, where its shape has a sequence a token: batch * n_new sequences of
- * one layer and one token).  pos: device [batch][n_new], the tokens' positions; they go to ret_pos where that is not NULL (pos may be NULL where neither needs it).
- * rotate != 0 (needs shape->rope_enabled, else VECTOR_ERR_SHAPE): the pair of channels (c, c + d/2) is turned by pos theta^(-2c/d), in fp32, before it is rounded.
- * A new row that the scale of its block does not hold makes the scale larger, and the rows that are there are rounded again; the first row of a block begins a new scale.
+ * New rows of every sequence's retained tier, from one generated token to a piece of a prompt, keys turned by their positions on the way.  ret_len[b] counts
+ * the new rows already: rows first_row[b] .. ret_len[b] - 1 (first_row and ret_len: as vector_block_tables wrote them), n_new at the most, are k_new[b][0],
+ * k_new[b][1], ...; a sequence with fewer has none of the others read.
+ * k_new, v_new: device [batch][n_new] rows of L * Hkv * d elements, k_stride and v_stride elements apart, so that they may be part of a wider row. 
+ * vector_norm_rope writes rows of this order, a token's heads behind one another, where its shape has a sequence a token: batch * n_new sequences of one
+ * layer and one token, Hkv times which is 65535 at the most.
+ * pos: device [batch][n_new], the tokens' positions; they go to ret_pos where that is not NULL (pos may be NULL where neither needs it).
+ * rotate != 0 (needs shape->rope_enabled, else VECTOR_ERR_SHAPE): the pair of channels (c, c + d/2) is turned by pos theta^(-2c/d), in fp32, before it is
+ * rounded.
+ * A new row that the scale of its block does not hold makes the scale larger, and the rows that are there are rounded again; the first row of a block begins
+ * a new scale.
  */
 VECTOR_API vector_status vector_append_q8(const vector_shape* shape, const vector_q8_cache* cache, const void* k_new, int64_t k_stride,
                                           const void* v_new, int64_t v_stride, int64_t n_new, const int32_t* first_row, const int32_t* pos,
@@ -500,10 +504,12 @@ VECTOR_API vector_status vector_read_q8(const vector_shape* shape, const vector_
 VECTOR_API size_t vector_decode_q8_workspace_bytes(const vector_shape* shape);
 
 /*
- * vector_decode_attn_q4 over the 8-bit pages: the same arguments, lengths read on the device, the same answers where rows are missing, and the same arithmetic: products of
- * stored rows are exact, sums fp32, weights and turned keys in fp16 (in two parts with fp32 queries or output).  The scale of a block's keys is a factor of its logits, that of its
- * values (and of key-only keys) one of the sums, which hold for the scale of the block before and change to the next one's.  A NaN in a key makes its unit's outputs NaN, one in a
- * value that channel's.  ws: at least vector_decode_q8_workspace_bytes() at a multiple of 256 bytes; calls that overlap on the GPU, two captured graphs' too, need workspaces of their own.
+ * vector_decode_attn_q4 over the 8-bit pages: the same arguments, lengths read on the device, the same answers where rows are missing, and the same
+ * arithmetic: products of stored rows are exact, sums fp32, weights and turned keys in fp16 (in two parts with fp32 queries or output).  The scale of a
+ * block's keys is a factor of its logits, that of its values (and of key-only keys) one of the sums, which hold for the scale of the block before and change
+ * to the next one's.  A NaN in a key makes its unit's outputs NaN, one in a value that channel's.
+ * ws: at least vector_decode_q8_workspace_bytes() at a multiple of 256 bytes; calls that overlap on the GPU, two captured graphs' too, need workspaces of
+ * their own.
  */
 VECTOR_API vector_status vector_decode_attn_q8(const vector_shape* shape, const void* q, const vector_q8_cache* cache, const void* W,
                                                void* out, int32_t out_dtype, void* ws, size_t ws_bytes, void* stream);

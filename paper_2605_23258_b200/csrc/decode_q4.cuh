@@ -1,26 +1,29 @@
 // The kernels of attention over the paged caches, in 4 bits (decode_q4.cu) and in 8 (decode_q8.cu).
 //
-// Streaming kernel.  A tile is a page of one unit: 64 keys and their values, or 64 key-only keys (8 bits: 32).  The sequence of all units' tiles, each
-// weighted by what it costs, is cut into equal contiguous ranges, one per warp: a warp is a worker of its own, which copies its tiles into
-// its own ring of slots (cp.async.bulk, one mbarrier a slot) and never waits for another warp.  It keeps one running state for a
-// unit's tier and writes it as a partial record when it leaves that.  The lengths lie on the device, so every block sums up the
-// sequences' costs itself.
+// Streaming kernel.  A tile is a page of one unit: 64 keys and their values, or 64 key-only keys (8 bits: 32).  The sequence of all units' tiles, each weighted
+// by what it costs, is cut into equal contiguous ranges, one per warp: a warp is a worker of its own, which copies its tiles into its own ring of slots
+// (cp.async.bulk, one mbarrier a slot) and never waits for another warp.  It keeps one running state for a unit's tier and writes it as a partial record when
+// it leaves that.  The lengths lie on the device, so every block sums up the sequences' costs itself.
 //
-// A worker takes 16 or 32 keys at a time.  A stored row's piece t is what lane t of a quad holds of a 16 x 16 fragment whose rows are keys: one 16-byte load (8 for
-// 64 channels) of codes and two scales a row, one conversion and one product for two channels, and no exchange between lanes:
+// A worker takes 16 or 32 keys at a time.  A stored row's piece t is what lane t of a quad holds of a 16 x 16 fragment whose rows are keys: one 16-byte load (8
+// for 64 channels) of codes and two scales a row, one conversion and one product for two channels, and no exchange between lanes:
 //   S^T = K Q^T    m16n8k16, keys down, the query heads across: no padding to sixteen rows of queries
 //   softmax        in fp32, against a reference that follows the maximum only when that has moved by more than SLACK (powers of two); the weights go to fp16, LEAD above one
 //   O^T += V^T P^T channels down, heads across; both operands are the registers at hand after an 8 x 8 transpose (movmatrix), and so are the key sums
 //                  A^T += K^T P^T of key-only keys, from the very registers that gave the logits
 // The sum of the weights is one more row of that product, a row of ones, so that a weight's rounding to fp16 is in numerator and denominator alike.
-// 8 bits: a row as fp16 is without its block's scale, a power of two.  That of keys is a factor of the tile's logits; that of values and of key-only keys is a factor
-// of the sums, which are kept for the scale of the tile before and multiplied, exactly, where the next one's is another.
-// Stored rows are exact in fp16, so the products are; halves of them too.  Queries are scaled by a power of two a head to fp16's range; fp32 queries take two fp16 parts.
-// EXACT (fp32 queries or fp32 output): weights, and keys turned back, in two fp16 parts, and sums of 16 keys added up outside the tensor cores,
-// which cut their sums off instead of rounding them.
+// 8 bits: a row as fp16 is without its block's scale, a power of two.  That of keys is a factor of the tile's logits; that of values and of key-only keys is a
+// factor of the sums, which are kept for the scale of the tile before and multiplied, exactly, where the next one's is another.
+// Stored rows are exact in fp16, so the products are; halves of them too.  Queries are scaled by a power of two a head to fp16's range; fp32 queries take two
+// fp16 parts.
+// EXACT (fp32 queries or fp32 output): weights, and keys turned back, in two fp16 parts, and sums of 16 keys added up outside the tensor cores, which cut their
+// sums off instead of rounding them.  bf16 queries with bf16 results take one part and the tensor cores' own fp32 sums, because the result's rounding hides
+// them: relative error (2-norm) against 64 bits over the 8-bit pages, with bf16's own rounding of the exact result in brackets, 640 units 0.001666 (0.001665),
+// 2048 units 0.001663 (0.001662), 472 units of rotary keys, turned in fp16, 0.001671 (0.001652).  Two parts take 77.9 us for the 54.9 of 128 units, with rotary
+// keys 163 for 82.
 //
-// Merge kernel.  A block combines the records of a unit, or of several sequences' units of one (layer, KV head), applies the map to the key sums on the
-// tensor cores (in three bf16 parts: 24 bits) and normalises.
+// Merge kernel.  A block combines the records of a unit, or of several sequences' units of one (layer, KV head), applies the map to the key sums on the tensor
+// cores (in three bf16 parts: 24 bits) and normalises.
 #ifndef VECTOR_DECODE_Q4_CUH_
 #define VECTOR_DECODE_Q4_CUH_
 
@@ -40,8 +43,8 @@ namespace dq4 {
 constexpr int MAX_BATCH = VECTOR_Q4_MAX_BATCH;
 // What a tile of either tier costs a worker, in small numbers.
 template <int RET, int APX> struct Costs { static constexpr int ret = RET, apx = APX, most = RET > APX ? RET : APX; };
-// A weight is 2^(logit - reference), and the reference is the largest logit so far less LEAD, or up to SLACK below that: weights reach 2^15 of fp16's range.  They have eleven bits
-// down to 2^-14, 2^-27 of the largest, and end at 2^-25, so that thousands of small weights count behind one key that takes nearly all.
+// A weight is 2^(logit - reference), and the reference is the largest logit so far less LEAD, or up to SLACK below that: weights reach 2^15 of fp16's range.
+// They have eleven bits down to 2^-14, 2^-27 of the largest, and end at 2^-25, so that thousands of small weights count behind one key that takes nearly all.
 // 640 units 183.3 us, 2048 units 127.5; LEAD 7 and SLACK 8, which moves the reference less often, 182.3 and 125.6.
 constexpr float LEAD = 13.f, SLACK = 2.f;
 static_assert(LEAD + SLACK <= 15.f, "weights are below 65504");
@@ -109,8 +112,11 @@ template <typename Cost> __device__ __forceinline__ int tile_from(int64_t r, int
 // FOLD: EXACT with at most four heads, whose first and second parts of weights are eight columns of one product.
 template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> struct Cfg {
     static_assert(EXACT || !FOLD, "one part needs no folding");
-    // 8 bits, us by 12 warps and by 16, which have 128 registers a thread: 64 channels, 512 units of up to 1700 and 3300 rows, fp32 results 51.2 and 46.5, bf16 48.4 and 45.0, rotary keys (472
-    // units, by the costs (2, 3)) 40.1 and 36.6; 128 channels 227 and 302.
+    // 8 bits, us by 12 warps and by 16, which have 128 registers a thread: 64 channels, 512 units of up to 1700 and 3300 rows, up to four heads and eight:
+    //                  bf16 results          fp32 results           fp32 queries and results
+    //                48.5 45.2, 49.9 46.0  51.1 46.6, 56.0 52.5   56.7 54.7, 62.0 60.5
+    //   rotary keys  69.3 61.5, 70.6 63.3  103.9 96.8, 112.1 103.8  112.0 106.1, 115.4 110.9
+    // although 16 warps spill where queries are fp32 or the heads of an fp32 result are not folded (up to 92 bytes); 128 channels, 640 units, 227 and 302.
     static constexpr int WARPS = EXACT && D == 128 && (!FOLD || ROPE || sizeof(T) == 4) ? 8 : F::SCALED && D == 64 ? 16 : 12;
     static constexpr int THREADS = 32 * WARPS;
     static constexpr int POS_AT = F::template TILE<D>;                 // of a key-only tile's positions, within an entry
@@ -123,17 +129,19 @@ template <typename T, int D, bool ROPE, bool EXACT, bool FOLD, class F = Bits4> 
     static constexpr float ROW_UNIT = ROPE && !F::SCALED ? .5f : 1.f;
     static constexpr int PAIRS = D / 8;                                // channel pairs of a lane in a row
     static constexpr int O_TILES = D / 16;
-    // Rows of a softmax step, in sixteens.  us by (retained, key-only), 128 units of 3000 and 6000 rows, four heads: 128 channels (2, 1) 44.4, (1, 1) 45.1, (2, 2) 46.1, fp32 results 47.4,
-    // 47.9, 49.8, rotary keys 70.8, 70.6, 80, with fp32 results, by the costs (2, 3), 150, 148, 207; 64 channels (2, 2) 32.8, (2, 1) 33.9, (1, 1) 34.1, fp32 results 34.8, 35.9, 36.7, rotary keys, which take
-    // (2, 1): 47.1 either way, 48.7.
-    // 8 bits, by steps of one and two sixteens of key-only rows: 64 units of 3277 and 6552 rows, eight heads, fp32 results of up to four heads and 128 channels 77.6 and 71.0,
-    // bf16 results 54.1 and 57.5, rotary keys 81.0 and 95.7, 64 channels 48.4 and 48.6.
+    // Rows of a softmax step, in sixteens.  us by (retained, key-only), 128 units of 3000 and 6000 rows, four heads: 128 channels (2, 1) 44.4, (1, 1) 45.1, (2,
+    // 2) 46.1, fp32 results 47.4, 47.9, 49.8, rotary keys 70.8, 70.6, 80, with fp32 results, by the costs (2, 3), 150, 148, 207; 64 channels (2, 2) 32.8, (2,
+    // 1) 33.9, (1, 1) 34.1, fp32 results 34.8, 35.9, 36.7, rotary keys, which take (2, 1): 47.1 either way, 48.7.
+    // 8 bits, by steps of one and two sixteens of key-only rows: 64 units of 3277 and 6552 rows, eight heads, fp32 results of up to four heads and 128 channels
+    // 77.6 and 71.0, bf16 results 54.1 and 57.5, rotary keys 81.0 and 95.7, 64 channels 48.4 and 48.6.
     static constexpr int N_RET = 2, N_APX = (D == 64 || (F::SCALED && FOLD && sizeof(T) == 2)) && !ROPE ? 2 : 1;
-    // What tiles of the tiers cost, (retained, key-only).  us for 128 units of 3000 and 6000 rows, four heads, 128 channels and 64: (4, 3) 44 and 33, (1, 1) 47 and 35, (2, 1) 48 and
-    // 34, (2, 3) 52 and 40; fp32 results 47 and 35, 50 and 37, 51 and 37, 55 and 42.  Rotary keys: (2, 3) 70.8 and 47.0, (1, 2) 70.3 and 52.6, (1, 1) 78 and 48, (4, 3) 81 and 49; fp32 results,
-    // turned in two parts: (1, 2) 140 and 76, (2, 3) 150 and 80, (1, 1) 171 and 88, (4, 3) 189 and 91.  fp32 queries and eight heads order them alike.
-    // 8 bits, rotary keys and 64 channels, 472 units of one ragged batch, 256 units of another and 128 of 3277 and 6552 rows: (4, 5) 34.8, 61.6 and 53.3, (2, 3) 36.6, 65.5 and 57.5, (1, 1) 35.6, 62.7 and 54.6,
-    // (5, 6) 34.9, 60.9 and 54.1; 128 channels, the first: (2, 3) 53.4, (4, 5) 55.0, (1, 1) 56.5, (1, 2) 58.4.  fp32 results, 64 channels, the first two: (1, 2) 51 and 97, (2, 3) 54 and 102, (1, 3) 57 and 112.
+    // What tiles of the tiers cost, (retained, key-only).  us for 128 units of 3000 and 6000 rows, four heads, 128 channels and 64: (4, 3) 44 and 33, (1, 1) 47
+    // and 35, (2, 1) 48 and 34, (2, 3) 52 and 40; fp32 results 47 and 35, 50 and 37, 51 and 37, 55 and 42.  Rotary keys: (2, 3) 70.8 and 47.0, (1, 2) 70.3 and
+    // 52.6, (1, 1) 78 and 48, (4, 3) 81 and 49; fp32 results, turned in two parts: (1, 2) 140 and 76, (2, 3) 150 and 80, (1, 1) 171 and 88, (4, 3) 189 and 91.
+    // fp32 queries and eight heads order them alike.
+    // 8 bits, rotary keys and 64 channels, 472 units of one ragged batch, 256 units of another and 128 of 3277 and 6552 rows: (4, 5) 34.8, 61.6 and 53.3, (2,
+    // 3) 36.6, 65.5 and 57.5, (1, 1) 35.6, 62.7 and 54.6, (5, 6) 34.9, 60.9 and 54.1; 128 channels, the first: (2, 3) 53.4, (4, 5) 55.0, (1, 1) 56.5, (1, 2)
+    // 58.4.  fp32 results, 64 channels, the first two: (1, 2) 51 and 97, (2, 3) 54 and 102, (1, 3) 57 and 112.
     using Cost = std::conditional_t<!ROPE, Costs<4, 3>, std::conditional_t<EXACT, Costs<1, 2>, std::conditional_t<F::SCALED && D == 64, Costs<4, 5>, Costs<2, 3>>>>;
 };
 
@@ -182,8 +190,8 @@ __device__ __forceinline__ uint32_t pack_weights(float lo, float hi) {
     asm("cvt.rn.satfinite.f16x2.f32 %0, %1, %2;\n" : "=r"(r) : "f"(hi), "f"(lo));
     return r;
 }
-// The reference for a largest logit, which is rounded: under LEAD below it by one or two of its last places, so that the logit itself, before its rounding, is never the lower
-// one.  From 2^28 on it could be by 16 and more, and no weight would be left.  An infinite one stays, and gives NaN.
+// The reference for a largest logit, which is rounded: under LEAD below it by one or two of its last places, so that the logit itself, before its rounding, is
+// never the lower one.  From 2^28 on it could be by 16 and more, and no weight would be left.  An infinite one stays, and gives NaN.
 __device__ __forceinline__ float reference(float top) { return top * (top > 0.f ? 1.f - 0x1p-23f : 1.f + 0x1p-23f) - LEAD; }
 __device__ __forceinline__ float2 unpack_h2(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
 
@@ -245,12 +253,13 @@ __device__ __forceinline__ void put_phase(TwoPhases& to, int which, unsigned lon
     to.turns[which] = (uint32_t)((phase + 0x80000000ull) >> 32);
     to.rest[which] = (float)(int32_t)(uint32_t)phase * 3.4061215800865545e-19f;      // 2 pi / 2^64
 }
-// Where the pair of channels 2 j, 2 j + 1 of piece tig's lies: what the four lanes of a quad read together is 64 bytes in a row (in the channels' order they met in one bank:
-// 128 units 70.9 us in place of 70.3).
+// Where the pair of channels 2 j, 2 j + 1 of piece tig's lies: what the four lanes of a quad read together is 64 bytes in a row (in the channels' order they
+// met in one bank: 128 units 70.9 us in place of 70.3).
 __device__ __forceinline__ constexpr int phase_place(int tig, int j) { return 4 * j + tig; }
-// Sine and cosine of a position times a phase.  Of the product modulo a turn the upper 23 bits count (8e-7): they become a number in [1, 2) and that a multiple of 2 pi
-// about zero, without a conversion from integers, which would wait for the unit that the sine and the cosine keep busy.  The phase's rest, under 2^-33 of a turn a position,
-// comes on top: 1e-4 at position 131072, 0.8 at 2^30 (16 sequences of 3000 and 6000 rows in 8 heads: 70.4 us, without it 67; by an integer product in its place 72.6).
+// Sine and cosine of a position times a phase.  Of the product modulo a turn the upper 23 bits count (8e-7): they become a number in [1, 2) and that a multiple
+// of 2 pi about zero, without a conversion from integers, which would wait for the unit that the sine and the cosine keep busy.  The phase's rest, under 2^-33
+// of a turn a position, comes on top: 1e-4 at position 131072, 0.8 at 2^30 (16 sequences of 3000 and 6000 rows in 8 heads: 70.4 us, without it 67; by an
+// integer product in its place 72.6).
 __device__ __forceinline__ void turn_cos_sin(uint32_t pos, float pos_f, uint32_t phase, float rest, float& cs, float& sn) {
     const float turns = __uint_as_float(((pos * phase) >> 9) ^ 0x3fc00000u);         // 1 + (angle + half a turn) modulo a turn
     __sincosf(fmaf(turns, 6.283185307179586f, fmaf(pos_f, rest, -9.42477796076938f)), &sn, &cs);
@@ -324,8 +333,11 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
     }
     if (threadIdx.x == 0) prefix[c.batch] = carry;
     __syncthreads();
-    // Where there is not work for all workers, a shorter range is over sooner and leaves the merge one more record: its steps go with the square root of a unit's tiles.  us by one, two, three,
-    // four tiles a range, 8 units of 20 tiles: 13.5, 13.6, 15.2, 16.8; of 81 tiles 16.6, 15.8, 16.7, 17.0, with rotary keys 18.4, 17.3, 19.5, 21.4; of 320 tiles 29.3, 24.6, 22.4, 22.7.
+    // Where there is not work for all workers, a shorter range is over sooner and leaves the merge one more record: its steps go with the square root of a
+    // unit's tiles.  us by one, two, three, four tiles a range, 8 units of 20 tiles: 13.5, 13.6, 15.2, 16.8; of 81 tiles 16.6, 15.8, 16.7, 17.0, with rotary
+    // keys 18.4, 17.3, 19.5, 21.4; of 320 tiles 29.3, 24.6, 22.4, 22.7.  By one tile and by this rule, contexts of 500, 2000, 8192 and 32768 tokens:
+    //   8 units   11.0 11.2, 13.4 13.6, 16.6 16.0, 29.2 22.8      32 units  12.3 12.4, 13.9 14.1, 17.8 17.0, 26.6 26.5
+    //   16 units  11.6 11.7, 13.5 13.7, 17.5 16.2, 24.9 24.0      64 and 128 units: up to 0.2 more by the rule, in 12.7 to 51.8
     int shortest = C::Cost::most;
     if constexpr (F::SCALED) shortest *= max((int)(.25f * sqrtf((float)carry / (float)(C::Cost::most * c.batch * c.LH)) + .5f), 1);
     const Deal deal(carry, gridDim.x * WARPS, shortest);
@@ -577,7 +589,8 @@ decode_q4_stream(const T* q, Cache c, int g, float scale_log2e, unsigned char* w
         }
     };
 
-    // The 16 rows at row0 turned back by their positions; lo: second parts.
+    // The 16 rows at row0 turned back by their positions; lo: second parts.  In one part, sines, cosines, products and turned keys are fp16, two channels an
+    // instruction.
     auto turn_back = [&](const unsigned char* tile, int row0, uint32_t (&x)[2][C::PAIRS], auto& lo) {
         int32_t pos[2];
 #pragma unroll
@@ -781,8 +794,8 @@ template <typename T, int D> struct MapTile {
     }
 };
 
-// A merge block's own shared memory beside the map, and how many blocks a multiprocessor holds: by registers four (bf16 maps) or three, by its 228 KB of shared memory, of which
-// the system takes one a block, two of fp32 maps of 128 channels (64 KB).
+// A merge block's own shared memory beside the map, and how many blocks a multiprocessor holds: by registers four (bf16 maps) or three, by its 228 KB of shared
+// memory, of which the system takes one a block, two of fp32 maps of 128 channels (64 KB).
 template <int D> constexpr int merge_shared() { return 2 * 8 * (D + 4) * 4 + 3 * 8 * 4 + 2 * 8 * MERGE_CHUNK * 4 + MERGE_CHUNK * 2 * 8 * 8; }
 template <typename T, int D, int THREADS> constexpr int merge_blocks() {
     constexpr int by_registers = THREADS == MERGE_MOST ? 1 : sizeof(T) == 2 ? 4 : 3, by_memory = 228 * 1024 / (MapTile<T, D>::BYTES + merge_shared<D>() + 1024);
@@ -856,8 +869,8 @@ decode_q4_merge(const unsigned char* ws, Cache c, int g, int seqs, int workers, 
                 for (int i = lane; i < 2 * n; i += 32) M = fmaxf(M, ml[i >> 1][i & 1][h].x);
                 M = warp_max(M);
                 float L = 0.f;
-                // An empty record has no sum either, and its numbers are not any.  One of logits that are all NaN has no reference, but a sum, which is NaN: its factor is
-                // zero or NaN, its numbers count.  So does one whose factor is zero because its logits are small.
+                // An empty record has no sum either, and its numbers are not any.  One of logits that are all NaN has no reference, but a sum, which is NaN:
+                // its factor is zero or NaN, its numbers count.  So does one whose factor is zero because its logits are small.
                 for (int i = lane; i < 2 * n; i += 32) {
                     const float2 x = ml[i >> 1][i & 1][h];
                     const bool empty = x.x == -INFINITY && x.y == 0.f;

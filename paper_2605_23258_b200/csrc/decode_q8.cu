@@ -1,5 +1,6 @@
-// Generation-time attention over the 8-bit paged cache (q8.cuh).  The kernels are those of the 4-bit pages, in decode_q4.cuh, with another kind of tile: a worker's chain of loads, products and softmax bounds
-// them, not the bytes (640 units of 3277 and 6552 rows, 1.1 GB, 227 us, of which copies alone take 198; at the copy rate 171).
+// Generation-time attention over the 8-bit paged cache (q8.cuh).  The kernels are those of the 4-bit pages, in decode_q4.cuh, with another kind of tile: a
+// worker's chain of loads, products and softmax bounds them, not the bytes (640 units of 3277 and 6552 rows, 1.1 GB, 227 us, of which copies alone take 198; at
+// the copy rate 171).
 #include "decode_q4.cuh"
 
 namespace vec {
@@ -44,8 +45,8 @@ struct Call {
                                               dm.g, seqs, workers, (const T*)W, out, out_dtype == VECTOR_BF16 ? 1 : 0));
         return VECTOR_OK;
     }
-    // As over the 4-bit pages, whose records are the same: no more units than multiprocessors take a large block each, more units small blocks, and as many sequences for a map that is fetched once as
-    // leave one round of blocks.
+    // As over the 4-bit pages, whose records are the same: no more units than multiprocessors take a large block each, more units small blocks, and as many
+    // sequences for a map that is fetched once as leave one round of blocks.
     template <typename T, int D, int HP> vector_status merge_heads(int workers) const {
         if (dm.U <= sm_count()) return merge_by<T, D, HP, MERGE_MOST>(1, workers);
         const int resident = merge_blocks<T, D, MERGE_THREADS>() * sm_count(), rounds = (dm.U + resident - 1) / resident;

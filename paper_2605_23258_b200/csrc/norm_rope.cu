@@ -1,12 +1,13 @@
-// From a layer's projections to the rows that this library takes: queries, keys and values of every token, heads behind one another, become a row a head, tokens
-// behind one another; on the way queries and keys are normed a head at a time and turned by their positions.
+// From a layer's projections to the rows that this library takes: queries, keys and values of every token, heads behind one another, become a row a head,
+// tokens behind one another; on the way queries and keys are normed a head at a time and turned by their positions.
 //
 //   y = x / sqrt(mean(x^2) + eps) * w,   then for each pair of channels (c, c + D/2) and t = pos theta^(-2c/D):   (y_c cos t - y' sin t, y' cos t + y_c sin t)
 //
-// A group of D / E lanes has a token and a run of heads of one projection, 16 bytes of a row a lane, several rows on their way at once: the factors of a channel, w cos t and (of the
-// pair's other channel, with its sign) w sin t, are computed once for the run, and a row then takes a sum of squares over its lanes, one exchange of its raw bytes with the lane half a
-// head away, two products and a factor a channel, two channels an instruction.  All in fp32, rounded once.  Bound by memory where there are many tokens (0.87 to 0.95 of the copy rate), by one
-// launch and the chain load, sum, store where there are few (64 tokens 3.4 us).
+// A group of D / E lanes has a token and a run of heads of one projection, 16 bytes of a row a lane, several rows on their way at once: the factors of a
+// channel, w cos t and (of the pair's other channel, with its sign) w sin t, are computed once for the run, and a row then takes a sum of squares over its
+// lanes, one exchange of its raw bytes with the lane half a head away, two products and a factor a channel, two channels an instruction.  All in fp32, rounded
+// once.  Bound by memory where there are many tokens (0.89 to 0.95 of the copy rate; 0.81 where the rows are over in 23 us), by one launch and the chain load,
+// sum, store where there are few (64 tokens 3.4 us).
 #include "common.cuh"
 #include "internal.h"
 #include "rope.cuh"
@@ -14,9 +15,10 @@
 namespace vec {
 namespace rows {
 
-// us for a prompt of 32768 tokens in 32 and 8 heads of 128 channels, window queries, keys and values (270 MB, 41.2 at the copy rate), and with all queries (805 MB, 123.2): 46.4 and 129.2;
-// blocks of 256 threads 50 and 155, four rows of a head on their way 46.1 and 130.7 (fp32, 64 channels: 22.9, eight 24.1), eight blocks a multiprocessor, which spill, 50 and 156, six 48 and 134;
-// angles and factors for every eight heads 46.5 and 140; both lanes of a pair computing all its angles, and products one at a time, 49 and 150.
+// us for a prompt of 32768 tokens in 32 and 8 heads of 128 channels, window queries, keys and values (270 MB, 41.2 at the copy rate), and with all queries (805
+// MB, 123.2): 46.4 and 129.2; blocks of 256 threads 50 and 155, four rows of a head on their way 46.1 and 130.7 (fp32, 64 channels: 22.9, eight 24.1), eight
+// blocks a multiprocessor, which spill, 50 and 156, six 48 and 134; angles and factors for every eight heads 46.5 and 140; both lanes of a pair computing all
+// its angles, and products one at a time, 49 and 150.
 constexpr int THREADS = 128;
 template <typename T> constexpr int AHEAD_OF = sizeof(T) == 2 ? 8 : 4;       // heads' rows that a lane has on their way
 template <typename T, int D> struct Lanes { static constexpr int E = 16 / (int)sizeof(T), N = D / E, GROUPS = THREADS / N; };

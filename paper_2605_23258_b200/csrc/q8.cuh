@@ -1,15 +1,16 @@
 // Rows in 8 bits, and the pages that hold them.
 //
-// A channel is an e4m3 number (sign, four exponent bits of bias 7, three mantissa bits, largest 448, no infinities) times 2^e, and a block of 32 tokens of
-// one (layer, KV head), its keys or its values, shares e: the smallest in [-32, 31] with 448 2^e >= max |x|.  Numbers within 2^14 of the block's largest
-// keep their four significant bits, so outlier channels cost the others nothing, and a power of two leaves the products of a block of rows exact: attention takes a row
-// as fp16 (one conversion for two channels, exact), and the factor once for a block.  Why one scale for many tokens: with a floating format it only has to put the block into range; a
-// scale a group of channels, as in the 4-bit pages, would cost a product for two channels in attention.  What is larger than 448 2^31 is cut off there, infinities too; a NaN stays one
-// channel's NaN and does not count for the scale.
+// A channel is an e4m3 number (sign, four exponent bits of bias 7, three mantissa bits, largest 448, no infinities) times 2^e, and a block of 32 tokens of one
+// (layer, KV head), its keys or its values, shares e: the smallest in [-32, 31] with 448 2^e >= max |x|.  Numbers within 2^14 of the block's largest keep their
+// four significant bits, so outlier channels cost the others nothing, and a power of two leaves the products of a block of rows exact: attention takes a row as
+// fp16 (one conversion for two channels, exact), and the factor once for a block.  Why one scale for many tokens: with a floating format it only has to put the
+// block into range; a scale a group of channels, as in the 4-bit pages, would cost a product for two channels in attention.  What is larger than 448 2^31 is
+// cut off there, infinities too; a NaN stays one channel's NaN and does not count for the scale.
 //
-// A page is such a block: for every (layer, KV head) a tile of 32 rows of D bytes, then 32 bytes of which the first is e + 32.  Order of a row: what lane t of a quad holds of a warp's
-// 16 x 16 matrix fragments is channels [t D/8, (t+1) D/8) and those half a head above them.  128 channels: as they are, but the halves of odd rows change places, so that the quads of two rows
-// that read 16 bytes a lane at once meet in no bank.  64 channels: a lane's two runs of eight bytes lie together.
+// A page is such a block: for every (layer, KV head) a tile of 32 rows of D bytes, then 32 bytes of which the first is e + 32.  Order of a row: what lane t of
+// a quad holds of a warp's 16 x 16 matrix fragments is channels [t D/8, (t+1) D/8) and those half a head above them.  128 channels: as they are, but the halves
+// of odd rows change places, so that the quads of two rows that read 16 bytes a lane at once meet in no bank.  64 channels: a lane's two runs of eight bytes
+// lie together.
 #ifndef VECTOR_Q8_CUH_
 #define VECTOR_Q8_CUH_
 

@@ -8,8 +8,8 @@
 namespace vec {
 namespace q8 {
 
-// us, 256 units of 13100 rows, 128 channels of bf16 (198 at the copy rate, either way): compaction 206, with the rows requested behind the table's answer and compared as fp32 numbers 290; reading
-// back 197, a run at a time 244.
+// us, 256 units of 13100 rows, 128 channels of bf16 (197 at the copy rate, either way): compaction 205, with the rows requested behind the table's answer and
+// compared as fp32 numbers 290; reading back 198, a run at a time 244.  fp32 (329) 328 and 444; 64 channels of bf16 (99) 128 and 119, of fp32 (164) 187 and 245.
 constexpr int THREADS = 128;
 
 // How a tile's rows are dealt to the threads: 16 bytes of a stored row each, E channels.
@@ -122,8 +122,8 @@ template <int N> __device__ __forceinline__ void largest(uint32_t (&most)[N], ui
         for (int w = 0; w < THREADS / 32; ++w) most[h] = max(most[h], shared[h][w]);
 }
 
-// Blocks of a unit: [0, br) retained keys, [br, 2 br) values, then key-only rows.  grid: (blocks, LH, batch).  The rows are on their way as soon as their indices are there, beside the
-// table and the length.
+// Blocks of a unit: [0, br) retained keys, [br, 2 br) values, then key-only rows.  grid: (blocks, LH, batch).  The rows are on their way as soon as their
+// indices are there, beside the table and the length.
 template <typename T, int D>
 __global__ void __launch_bounds__(THREADS)
 compact_kernel(const T* K, const T* V, int64_t N, const int32_t* ret_idx, const int32_t* apx_idx, int n_ret, int n_apx, Pools pools) {
@@ -171,8 +171,8 @@ compact_kernel(const T* K, const T* V, int64_t N, const int32_t* ret_idx, const 
     if (threadIdx.x == 0) place.tile[Row<D>::SCALE_AT] = (unsigned char)(e - LOW);
 }
 
-// Rows [first_row[b], ret_len[b]) of a sequence, n_new at the most, into the blocks that they touch, HEADS neighbouring heads a thread block, whose angles are computed once.
-// grid: (touched blocks x 2, LH / HEADS, batch).
+// Rows [first_row[b], ret_len[b]) of a sequence, n_new at the most, into the blocks that they touch, HEADS neighbouring heads a thread block, whose angles are
+// computed once.  grid: (touched blocks x 2, LH / HEADS, batch).
 template <typename T, int D, bool ROTATE, int HEADS>
 __global__ void __launch_bounds__(THREADS)
 append_kernel(const T* k_new, int64_t k_stride, const T* v_new, int64_t v_stride, int n_new, const int32_t* first_row, const int32_t* pos, Pools pools, RopePhases phases) {
@@ -355,8 +355,11 @@ struct AppendCall {
                                               pools, ph));
         return VECTOR_OK;
     }
-    // us by one head a thread block and by two, 2048 rows of four sequences in 8 heads: bf16 turned 19.7 and 17.3, not turned 11.3 and 11.9, 64 channels turned 11.3 and 8.8, fp32 turned
-    // 23.1 and 20.9, not turned 16.0 and 34.6; a row of 32 sequences 3.7 either way.
+    // us by one head a thread block and by two, turned, in 8 heads: 2048 rows of four sequences (7.7 at the copy rate; not turned 11.3 and 11.9), 64 rows of 32,
+    // 300 of one, 5 rows and one row of 32:
+    //   bf16, 128 channels  19.7 17.3, 8.1 7.0, 4.0 3.9, 3.9 3.8, 3.3 3.4     64 channels  11.8 9.1, 5.4 5.4, 3.3 3.2, 3.3 3.2, 3.3 3.2
+    //   fp32, 128 channels  23.2 21.0, 9.2 8.4, 4.6 5.1, 4.5 4.8, 4.1 4.0     64 channels  13.5 11.2, 5.7 6.1, 3.3 3.2, 3.3 3.2, 3.3 3.2
+    // fp32 not turned 16.0 and 34.6.
     template <typename T, int D> vector_status run() const {
         if (!rotate) return put<T, D, false, 1>();
         return dm.LH % 2 == 0 ? put<T, D, true, 2>() : put<T, D, true, 1>();
