@@ -741,9 +741,12 @@ def vector_decode_attn_q4(shape: Shape, q, cache: Q4Cache, W, out, ws=None, stre
 # ---- the mixed cache in 8 bits and pages
 def _on_current_device(*tensors):
     """The calls run on the current device: a tensor of another one is refused."""
+    here = None                                           # a CPU tensor's call is refused without asking for it
     for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
-            raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+        if t is not None and t.is_cuda:
+            here = torch.cuda.current_device() if here is None else here
+            if t.get_device() != here:
+                raise ValueError(f"a tensor lies on {t.device}, the current device is cuda:{here}")
 
 
 def _of_cache(cache: Q8Cache):

@@ -232,7 +232,7 @@ class PagedCache:
             if pos is None and (rotate or self.cache.ret_pos is not None):
                 raise ValueError("pos is missing")
             B._positions(pos, sh.batch * n)
-            B._on_current_device(k_new, v_new, pos, *B._of_cache(self.cache))
+            B._on_current_device(k_new, v_new, pos, self.cache.ret_pages)      # the cache's tensors were made on one device; asking each of them took 2 us
             self._change("ret", self.active if n == 1 else self.active * n)
             B.vector_append_q8(self.shape, self.cache, k_new, v_new, self.first_row, pos, rotate)
             return

@@ -79,3 +79,16 @@ def test_lengths_and_pages_are_as_they_were():
         assert not paged.cache.ret_len.any() and paged.free_pages() == (8, 8)
         paged.append(dense, dense, pos)
         assert paged.cache.ret_len.tolist() == [3] * batch and paged.free_pages() == (8 - batch, 8)
+
+
+def test_a_cache_of_another_device(changes):
+    """The current device is another one than the cache's, whose tensors were made together."""
+    paged = _paged()
+    paged.cache.ret_pages = _on(paged.cache.ret_pages, 1)
+    x, pos = _on(torch.zeros(2, 3, 256, dtype=BF)), _on(torch.zeros(2, 3, dtype=torch.int32))
+    with pytest.raises(ValueError, match="device"):
+        paged.append(x, x, pos)
+    comp = Compressor(vec.Shape(1, 1, 4, 2, 128, vec.VECTOR_BF16, 16), vec.vector_plan_budget(150, 60, -1, 16), device="cpu")
+    with pytest.raises(ValueError, match="device"):
+        paged.admit(0, comp, *(_on(torch.zeros(2, 150, 128, dtype=BF)) for _ in range(2)))
+    assert not changes
