@@ -834,7 +834,7 @@ def vector_compact_q8(shape: Shape, budget: Budget, K, V, ret_idx, apx_idx, cach
 def vector_append_q8(shape: Shape, cache: Q8Cache, k_new, v_new, first_row, pos=None, rotate: bool = False, stream=None):
     """k_new, v_new [batch][n] rows of L * Hkv * d elements: rows first_row[b] .. cache.ret_len[b] - 1 of every sequence, keys turned by pos [batch][n] where `rotate`.
     Of several tokens the first two dimensions are [batch][n], or the only two [batch * n][L * Hkv * d].  vector_norm_rope leaves rows of this order where its shape has a sequence a token
-    (batch * n sequences of one layer and one token, pos [batch * n])."""
+    (batch * n sequences of one layer and one token, pos [batch * n]): its k_out.view(batch, n, -1)."""
     rc = (_marshal_module or _marshal()).append_q8(shape, cache, k_new, v_new, first_row, pos, rotate, _handle(stream))
     if rc is not None:
         if rc:
